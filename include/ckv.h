@@ -365,8 +365,8 @@ CKV_API ckv_status ckv_set_wait_limit_us(uint32_t microseconds);
 /* Synchronises `stream`, then returns the workspace's device status: *code = 0 if no kernel
  * recorded an error since the last reset, else the first error (1 = cu_seqlens_dev disagrees
  * with the host copy, 2 = a wait timed out, 3 = an index out of range, 4 = a window row's
- * largest logit beyond +-680, which the two-pass kernel's fp64 row sums cannot hold); *detail
- * says where.
+ * largest logit beyond +-680, which the two-pass kernel's fp64 row sums cannot hold, 5 =
+ * ckv_block_tables: the new tokens do not fit); *detail says where.
  * With reset != 0 the status word is cleared afterwards. */
 CKV_API ckv_status ckv_read_device_status(void* workspace, ckv_stream stream, int32_t reset,
                                   int32_t* code, int32_t* detail);
@@ -401,6 +401,105 @@ CKV_API ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer,
                                            const void* k, int64_t tok_stride,
                                            int64_t head_stride, float* scores,
                                            int32_t* status_out, ckv_stream stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Around the compression: the prefill attention that hands over the window rows' lse, a paged cache
+ * for the kept rows and the tokens that follow, and the attention of new tokens over it.  A layer's
+ * way through them: ckv_prefill_attention -> ckv_compress_layer(s)_lse (with its lse_win) ->
+ * ckv_block_tables (the kept lengths) -> ckv_cache_write (k_out, v_out); then per decode step
+ * ckv_block_tables -> ckv_cache_write -> ckv_paged_attention.  (The paper's own decoding over the
+ * compressed cache is Eq. 3-4; its prefill attention is Eq. 2.)
+ *
+ * The workspace of these calls is ckv_attention_workspace_size's, zeroed once like the others; the
+ * rules above for workspaces, streams, alignment and errors hold.  Of the config they read the head
+ * counts, window, softmax_scale and max_ctas.  fp32 logits, sums and outputs' accumulation; the
+ * softmax's numerators are rounded to bf16 for the product with v, as the outputs are at the end.
+ * Logits are below 1e8 in magnitude.  v is finite: a NaN or an infinity in a value row can reach query
+ * rows of its sequence that stand less than 256 tokens before it, never another sequence.  What a query
+ * row does not see of k may be anything. */
+
+CKV_API ckv_status ckv_attention_workspace_size(const ckv_config* cfg, size_t* bytes);
+
+/* Causal attention of packed prompts (Eq. 2): query row i of a sequence sees its keys 0..i,
+ *   out[t, h] = sum_j exp(scale * q_t,h . k_j - lse[h, t]) v_j.
+ *   q    [T, H_q, 128] with strides in elements (0 = packed), multiples of 8
+ *   k, v [T, H_kv, 128], tok_stride / head_stride as elsewhere
+ *   out  [T, H_q, 128] packed; not q, k or v
+ *   lse      fp32, natural log, lse[h * lse_head_stride + t] (stride >= T, 0 = T); may be NULL
+ *   lse_win  the last w rows of every sequence, lse_win[h * lse_win_head_stride + s * w + r], row r
+ *            at position L_s - w + r (stride >= S * w, 0 = S * w): what the _lse calls take; rows
+ *            before the sequence start are not written; may be NULL
+ * Sequences may be empty. */
+CKV_API ckv_status ckv_prefill_attention(const ckv_config* cfg, const ckv_batch* batch, const void* q,
+                                         int64_t q_tok_stride, int64_t q_head_stride, const void* k,
+                                         const void* v, int64_t tok_stride, int64_t head_stride,
+                                         void* out, float* lse, int64_t lse_head_stride,
+                                         float* lse_win, int64_t lse_win_head_stride, void* workspace,
+                                         size_t workspace_bytes, ckv_stream stream);
+
+/* A paged cache of one or more layers: pages of page_size tokens, [num_pages][page_size, H_kv, 128]
+ * bf16, page p at element p * page_stride (0 = packed; a multiple of 8).  Slot i is token
+ * i % page_size of page i / page_size.  Rows of a page behind a sequence's end are never used, so
+ * pages need no clearing. */
+typedef struct ckv_paged_cache {
+    void* k_pages;
+    void* v_pages;
+    int64_t page_stride;
+    int32_t num_pages;
+    int32_t page_size; /* 16, 32, 64 or 128 */
+} ckv_paged_cache;
+
+/* Block tables and slot maps from the rows' lengths, on the GPU (nothing is read back, so a decode
+ * step that calls this can be captured and replayed).  A row is one sequence, or one (layer,
+ * sequence) where the layers keep different lengths.
+ *   cache_lens [num_rows]  tokens that the row holds
+ *   new_lens   [num_rows]  tokens to append (0: none); -1: the row's pages are given back and its
+ *                          length becomes 0 (for later calls: this call does not hand them out)
+ *   free_pages [num_pages] ring of page indices; pool[0] and pool[1] count the pages ever taken and
+ *                          ever returned, so that entries pool[0]..pool[1]-1 (mod num_pages) are free:
+ *                          at the start all page indices and {0, num_pages}
+ *   block_table [num_rows][max_blocks]  the entries of the row's new pages are written (pages are
+ *                          taken in row order), the others left
+ *   slot_map   [num_slots] out: the new tokens' slots, row after row; -1 behind the last one
+ *   cu_new     [num_rows+1] out: first new token of each row
+ *   lens_out, pool_out     out: the new lengths and counters; may be cache_lens and pool themselves
+ * All device memory, not overlapping otherwise.  If the new tokens do not fit (a length is negative,
+ * new_lens below -1, a row longer than max_blocks pages, more tokens than num_slots, too few free
+ * pages, counters out of order), nothing is taken or given back: cu_new is 0, slot_map -1, lengths and
+ * counters stay, and the status word gets code 5 with detail 1 (a row), 2 (num_slots), 3 (counters) or
+ * 4 (pages).  A page index outside [0, num_pages) gives slot -1 and code 3. */
+CKV_API ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* cache_lens,
+                                    const int32_t* new_lens, int32_t* free_pages, int32_t num_pages,
+                                    const int64_t* pool, int32_t* block_table, int32_t max_blocks,
+                                    int32_t* slot_map, int32_t num_slots, int32_t* cu_new,
+                                    int32_t* lens_out, int64_t* pool_out, void* workspace,
+                                    size_t workspace_bytes, ckv_stream stream);
+
+/* Rows into the cache: token t of k, v [num_tokens, H_kv, 128] goes to slot slot_map[t] (device);
+ * -1 is skipped, any other slot outside the cache is skipped and gives status code 3.  Bit copy.
+ * The slots of a call are distinct. */
+CKV_API ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache* cache,
+                                   int32_t num_tokens, const void* k, const void* v,
+                                   int64_t tok_stride, int64_t head_stride, const int32_t* slot_map,
+                                   void* workspace, size_t workspace_bytes, ckv_stream stream);
+
+/* Attention of new tokens over the paged cache: single tokens, or chunks of them.  Sequence s has n =
+ * cu_new[s+1] - cu_new[s] query rows (q rows cu_new[s] - cu_new[0] on) and L = cache_lens[s] cached
+ * tokens, the new ones included and written before; its query row i sees keys 0..L - n + i, key j in
+ * page block_table[s * max_blocks + j / page_size].  All lengths are read on the device: a captured
+ * call can be replayed as they grow.
+ *   q, out [num_tokens, H_q, 128], lse [H_q][lse_head_stride] (stride >= num_tokens) as for
+ *   ckv_prefill_attention.  Rows from cu_new[num_seqs] - cu_new[0] on (padding) are left as they were.
+ * Status code 3: cu_new that decreases or runs past num_tokens (then nothing is written); a sequence
+ * with L < n or L beyond its table row (its rows are not written), or with a page outside the cache
+ * (its rows are undefined). */
+CKV_API ckv_status ckv_paged_attention(const ckv_config* cfg, const ckv_paged_cache* cache,
+                                       int32_t num_seqs, int32_t num_tokens,
+                                       const int32_t* block_table, int32_t max_blocks,
+                                       const int32_t* cache_lens, const int32_t* cu_new, const void* q,
+                                       int64_t q_tok_stride, int64_t q_head_stride, void* out,
+                                       float* lse, int64_t lse_head_stride, void* workspace,
+                                       size_t workspace_bytes, ckv_stream stream);
 
 #ifdef __cplusplus
 }

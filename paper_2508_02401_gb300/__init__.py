@@ -25,6 +25,8 @@ __all__ = [
     "ckv_compress_layer_lse", "ckv_semantic_retrieval_scores", "ckv_set_wait_limit_us",
     "new_workspace", "new_outputs", "LayerIO", "ckv_workspace_size_layers", "ckv_score_windows",
     "ckv_compress_layers", "ckv_compress_layers_lse", "new_layers_workspace", "ckv_score_windows_lse",
+    "PagedCache", "new_paged_cache", "new_attention_workspace", "ckv_attention_workspace_size",
+    "ckv_prefill_attention", "ckv_block_tables", "ckv_cache_write", "ckv_paged_attention",
 ]
 
 POOL_MAX, POOL_AVG = 0, 1
@@ -71,6 +73,11 @@ class _Batch(C.Structure):
                 ("cu_seqlens_dev", C.c_void_p)]
 
 
+class _PagedCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64),
+                ("num_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
 def load():
     """Loads libckv.so (built by ``paper_2508_02401_gb300.build``)."""
     global _lib
@@ -82,7 +89,7 @@ def load():
                           "`python -c 'import __graft_entry__ as g; g.build()'`")
     lib = C.CDLL(path)
     P, I32, I64, SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
-    cfg, bat = C.POINTER(_Config), C.POINTER(_Batch)
+    cfg, bat, cache = C.POINTER(_Config), C.POINTER(_Batch), C.POINTER(_PagedCache)
     sigs = {
         "ckv_abi_version": ([], I32),
         "ckv_status_string": ([C.c_int], C.c_char_p),
@@ -110,6 +117,11 @@ def load():
         "ckv_score_windows_lse": ([cfg, I32, P, bat, P, SZ, P], C.c_int),
         "ckv_compress_layers": ([cfg, I32, P, bat, P, SZ, P], C.c_int),
         "ckv_compress_layers_lse": ([cfg, I32, P, bat, P, SZ, P], C.c_int),
+        "ckv_attention_workspace_size": ([cfg, C.POINTER(SZ)], C.c_int),
+        "ckv_prefill_attention": ([cfg, bat, P, I64, I64, P, P, I64, I64, P, P, I64, P, I64, P, SZ, P], C.c_int),
+        "ckv_block_tables": ([I32, I32, P, P, P, I32, P, P, I32, P, I32, P, P, P, P, SZ, P], C.c_int),
+        "ckv_cache_write": ([cfg, cache, I32, P, P, I64, I64, P, P, SZ, P], C.c_int),
+        "ckv_paged_attention": ([cfg, cache, I32, I32, P, I32, P, P, P, I64, I64, P, P, I64, P, SZ, P], C.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -449,3 +461,173 @@ def new_outputs(cfg, layer, batch, device="cuda"):
     k_out = torch.empty((tk, cfg.num_kv_heads, cfg.head_dim), dtype=torch.bfloat16, device=device)
     v_out = torch.empty_like(k_out)
     return idx, cu_keep_dev, k_out, v_out, cu_keep
+
+
+# ------------------------------------------------------------------ attention and the paged cache
+def _need(name, t, dtype, numel=None):
+    """The calls below read and write whole tensors by their sizes, so a tensor of another type, device
+    or size would be read out of bounds: ValueError instead."""
+    import torch
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    if numel is not None and t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} values, {numel} are needed")
+
+
+def _need_packed(name, t, dtype, numel):
+    _need(name, t, dtype, numel)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+
+
+def _need_rows(name, t, heads, tok_stride, head_stride):
+    """A [T, heads, 128] bfloat16 tensor; its strides are the ones given, or packed."""
+    import torch
+    _need(name, t, torch.bfloat16)
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not [T, {heads}, 128]")
+    want = (tok_stride or heads * 128, head_stride or 128, 1)
+    if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
+        raise ValueError(f"{name} has strides {t.stride()}, the call says {want}")
+
+
+class PagedCache:
+    """K and V pages [num_pages, page_size, H_kv, 128] bfloat16 (ckv_paged_cache).  The pages may be
+    strided (one buffer [num_pages, 2, page_size, H_kv, 128] for both); a page is packed."""
+
+    def __init__(self, k_pages, v_pages):
+        import torch
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            _need(name, t, torch.bfloat16)
+            if t.dim() != 4 or t.shape[3] != 128 or t.shape != k_pages.shape or t.stride() != k_pages.stride():
+                raise ValueError("k_pages and v_pages are [num_pages, page_size, H_kv, 128] of the same strides")
+            if t.numel() and t.stride()[1:] != (t.shape[2] * 128, 128, 1):
+                raise ValueError(f"{name}: a page is not packed")
+        self.k_pages, self.v_pages = k_pages, v_pages
+        # (of a single page torch may give any stride)
+        stride = k_pages.stride(0) if k_pages.shape[0] > 1 else 0
+        self._c = _PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), stride, k_pages.shape[0], k_pages.shape[1])
+
+    @property
+    def page_size(self) -> int:
+        return self.k_pages.shape[1]
+
+    @property
+    def num_pages(self) -> int:
+        return self.k_pages.shape[0]
+
+    @property
+    def ref(self):
+        return C.byref(self._c)
+
+
+def new_paged_cache(cfg, num_pages, page_size, device="cuda"):
+    """A PagedCache of uninitialised pages."""
+    import torch
+    shape = (num_pages, page_size, cfg.num_kv_heads, 128)
+    return PagedCache(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
+def ckv_attention_workspace_size(cfg) -> int:
+    n = C.c_size_t(0)
+    _check(load().ckv_attention_workspace_size(cfg.ref, C.byref(n)), "ckv_attention_workspace_size")
+    return n.value
+
+
+def new_attention_workspace(cfg, device="cuda"):
+    """A zeroed workspace for the attention and paged-cache calls (uint8 tensor)."""
+    import torch
+    return torch.zeros(ckv_attention_workspace_size(cfg), dtype=torch.uint8, device=device)
+
+
+def ckv_prefill_attention(cfg, batch, q, k, v, out, workspace, lse=None, lse_win=None, lse_head_stride=0,
+                          lse_win_head_stride=0, stream=None, q_tok_stride=0, q_head_stride=0,
+                          tok_stride=0, head_stride=0):
+    """Causal attention of packed prompts; lse [H_q, T] and lse_win [H_q, S*w] (what the _lse calls
+    take) are written where given."""
+    import torch
+    T, Hq, f32 = batch.total_tokens, cfg.num_q_heads, torch.float32
+    _need_rows("q", q, Hq, q_tok_stride, q_head_stride)
+    for name, t in (("k", k), ("v", v)):
+        _need_rows(name, t, cfg.num_kv_heads, tok_stride, head_stride)
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.shape[0] < T:
+            raise ValueError(f"{name} holds {t.shape[0]} tokens, the batch {T}")
+    _need_packed("out", out, torch.bfloat16, T * Hq * 128)
+    if lse is not None:
+        _need_packed("lse", lse, f32, (Hq - 1) * (lse_head_stride or T) + T)
+    if lse_win is not None:
+        rows = batch.num_seqs * cfg.window
+        _need_packed("lse_win", lse_win, f32, (Hq - 1) * (lse_win_head_stride or rows) + rows)
+    _check(load().ckv_prefill_attention(cfg.ref, batch.ref, _ptr(q), q_tok_stride, q_head_stride, _ptr(k),
+                                        _ptr(v), tok_stride, head_stride, _ptr(out), _ptr(lse),
+                                        lse_head_stride, _ptr(lse_win), lse_win_head_stride,
+                                        _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream(stream)), "ckv_prefill_attention")
+
+
+def ckv_block_tables(page_size, cache_lens, new_lens, free_pages, pool, block_table, slot_map, cu_new,
+                     lens_out, pool_out, workspace, stream=None):
+    """Appends new_lens tokens to every row (-1: gives its pages back): block_table [rows, max_blocks],
+    slot_map, cu_new [rows + 1], lens_out and pool_out are written (int32; pool int64 [2])."""
+    import torch
+    n, i32 = cache_lens.numel(), torch.int32
+    for name, t, size in (("cache_lens", cache_lens, n), ("new_lens", new_lens, n), ("free_pages", free_pages, 1),
+                          ("block_table", block_table, n), ("slot_map", slot_map, 0), ("cu_new", cu_new, n + 1),
+                          ("lens_out", lens_out, n)):
+        _need_packed(name, t, i32, size)
+    for name, t in (("pool", pool), ("pool_out", pool_out)):
+        _need_packed(name, t, torch.int64, 2)
+    if block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError(f"block_table is {tuple(block_table.shape)}, not [{n}, max_blocks]")
+    _check(load().ckv_block_tables(page_size, n, _ptr(cache_lens), _ptr(new_lens), _ptr(free_pages),
+                                   free_pages.numel(), _ptr(pool), _ptr(block_table), block_table.shape[1],
+                                   _ptr(slot_map), slot_map.numel(), _ptr(cu_new), _ptr(lens_out),
+                                   _ptr(pool_out), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)),
+           "ckv_block_tables")
+
+
+def _need_cache(cfg, cache):
+    if cache.k_pages.shape[2] != cfg.num_kv_heads:
+        raise ValueError(f"the cache has {cache.k_pages.shape[2]} KV heads, the config {cfg.num_kv_heads}")
+
+
+def ckv_cache_write(cfg, cache, k, v, slot_map, workspace, stream=None, tok_stride=0, head_stride=0):
+    """k, v [tokens, H_kv, 128] into the cache's slots slot_map [tokens] int32 (-1: skipped)."""
+    import torch
+    _need_cache(cfg, cache)
+    n = slot_map.numel()
+    _need_packed("slot_map", slot_map, torch.int32, n)
+    for name, t in (("k", k), ("v", v)):
+        _need_rows(name, t, cfg.num_kv_heads, tok_stride, head_stride)
+        if t.shape[0] < n:
+            raise ValueError(f"{name} holds {t.shape[0]} tokens, slot_map {n}")
+    _check(load().ckv_cache_write(cfg.ref, cache.ref, n, _ptr(k), _ptr(v), tok_stride, head_stride,
+                                  _ptr(slot_map), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _stream(stream)),
+           "ckv_cache_write")
+
+
+def ckv_paged_attention(cfg, cache, block_table, cache_lens, cu_new, q, out, workspace, lse=None,
+                        lse_head_stride=0, stream=None, q_tok_stride=0, q_head_stride=0):
+    """Attention of the new tokens q [tokens, H_q, 128] over the cache: block_table [S, max_blocks],
+    cache_lens [S] (new tokens included), cu_new [S + 1] int32, all read on the device."""
+    import torch
+    _need_cache(cfg, cache)
+    S, Hq, T, i32 = cache_lens.numel(), cfg.num_q_heads, q.shape[0], torch.int32
+    _need_rows("q", q, Hq, q_tok_stride, q_head_stride)
+    for name, t, size in (("block_table", block_table, S), ("cache_lens", cache_lens, S), ("cu_new", cu_new, S + 1)):
+        _need_packed(name, t, i32, size)
+    if block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError(f"block_table is {tuple(block_table.shape)}, not [{S}, max_blocks]")
+    _need_packed("out", out, torch.bfloat16, T * Hq * 128)
+    if lse is not None:
+        _need_packed("lse", lse, torch.float32, (Hq - 1) * (lse_head_stride or T) + T)
+    _check(load().ckv_paged_attention(cfg.ref, cache.ref, S, T, _ptr(block_table), block_table.shape[1],
+                                      _ptr(cache_lens), _ptr(cu_new), _ptr(q), q_tok_stride, q_head_stride,
+                                      _ptr(out), _ptr(lse), lse_head_stride, _ptr(workspace),
+                                      workspace.numel() * workspace.element_size(), _stream(stream)),
+           "ckv_paged_attention")

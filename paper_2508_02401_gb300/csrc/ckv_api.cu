@@ -1609,6 +1609,286 @@ ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer, const c
     return CKV_OK;
 }
 
+// ---------------------------------------------------------------------- attention, paged cache
+namespace {
+
+// The workspace of the attention and paged-cache calls: the status header, the counters of split
+// units, block_tables' ticket, then the partial results of split units.
+struct AttnWs {
+    size_t counters, ticket, partials, total;
+};
+AttnWs attn_ws_layout() {
+    AttnWs l;
+    l.counters = sizeof(WsHeader);
+    l.ticket = l.counters + kAttnMaxCtas * sizeof(int);
+    l.partials = round_up(l.ticket + sizeof(int), kWsAlign);
+    l.total = l.partials + static_cast<size_t>(kAttnMaxCtas) * 2 * attn_partial_floats() * sizeof(float);
+    return l;
+}
+
+ckv_status check_attn_ws(void* ws, size_t bytes, AttnWs* l) {
+    *l = attn_ws_layout();
+    if (!ws) return fail(CKV_ERR_WORKSPACE, "workspace is NULL");
+    if (!aligned(ws, kWsAlign)) return fail(CKV_ERR_WORKSPACE, "workspace not 256-byte aligned");
+    if (bytes < l->total)
+        return fail(CKV_ERR_WORKSPACE, "workspace %zu bytes < required %zu", bytes, l->total);
+    return CKV_OK;
+}
+
+// Strides of a [T, heads, 128] tensor: 0 = packed, else positive multiples of 8 elements (16 bytes).
+ckv_status check_strides(const char* name, int heads, int64_t* tok, int64_t* head) {
+    if (*tok == 0) *tok = static_cast<int64_t>(heads) * kHeadDim;
+    if (*head == 0) *head = kHeadDim;
+    if (*tok < 0 || *head < 0 || *tok % 8 || *head % 8)
+        return fail(CKV_ERR_INVALID_ARG, "%s strides must be non-negative multiples of 8 elements", name);
+    if (*tok >= (static_cast<int64_t>(1) << 38) || *head >= (static_cast<int64_t>(1) << 38))
+        return fail(CKV_ERR_UNSUPPORTED, "%s stride too large", name);
+    return CKV_OK;
+}
+
+ckv_status check_lse_out(const char* name, float* lse, int64_t least, int64_t* stride) {
+    if (!lse) return CKV_OK;
+    if (!aligned(lse, 4)) return fail(CKV_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+    if (*stride == 0) *stride = least;
+    if (*stride < least)
+        return fail(CKV_ERR_INVALID_ARG, "%s head stride %lld < %lld", name, static_cast<long long>(*stride),
+                    static_cast<long long>(least));
+    return CKV_OK;
+}
+
+ckv_status check_cache(const ckv_paged_cache* c, int64_t* page_stride) {
+    if (!c) return fail(CKV_ERR_INVALID_ARG, "cache is NULL");
+    if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+        return fail(c->page_size < 1 ? CKV_ERR_INVALID_ARG : CKV_ERR_UNSUPPORTED,
+                    "page_size %d (16, 32, 64 or 128)", c->page_size);
+    if (c->num_pages < 1) return fail(CKV_ERR_INVALID_ARG, "num_pages %d < 1", c->num_pages);
+    if (static_cast<int64_t>(c->num_pages) * c->page_size > INT_MAX - 128)
+        return fail(CKV_ERR_UNSUPPORTED, "more than 2^31 - 129 slots");
+    if (!c->k_pages || !c->v_pages) return fail(CKV_ERR_INVALID_ARG, "k_pages and v_pages are required");
+    if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16))
+        return fail(CKV_ERR_INVALID_ARG, "k_pages or v_pages is not 16-byte aligned");
+    *page_stride = c->page_stride;
+    return CKV_OK;
+}
+
+ckv_status resolve_page_stride(const ckv_paged_cache* c, int Hkv, int64_t* page_stride) {
+    const int64_t least = static_cast<int64_t>(c->page_size) * Hkv * kHeadDim;
+    if (*page_stride == 0) *page_stride = least;
+    if (*page_stride < least || *page_stride % 8)
+        return fail(CKV_ERR_INVALID_ARG, "page_stride %lld: a multiple of 8 elements, at least %lld",
+                    static_cast<long long>(*page_stride), static_cast<long long>(least));
+    if (*page_stride >= (static_cast<int64_t>(1) << 38)) return fail(CKV_ERR_UNSUPPORTED, "page_stride too large");
+    return CKV_OK;
+}
+
+ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
+    const cudaError_t e = launch_attention(L, stream);
+    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
+}
+
+void attn_common(AttnLaunch& L, const ckv_config* cfg, void* workspace, const AttnWs& l) {
+    uint8_t* w8 = static_cast<uint8_t*>(workspace);
+    L.Hq = cfg->num_q_heads;
+    L.Hkv = cfg->num_kv_heads;
+    L.w = cfg->window;
+    L.max_ctas = cfg->max_ctas;
+    L.scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf(static_cast<float>(kHeadDim));
+    L.status = static_cast<int*>(workspace);
+    L.counters = reinterpret_cast<int*>(w8 + l.counters);
+    L.partials = reinterpret_cast<float*>(w8 + l.partials);
+}
+
+}  // namespace
+
+ckv_status ckv_attention_workspace_size(const ckv_config* cfg, size_t* bytes) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    if (!bytes) return fail(CKV_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = attn_ws_layout().total;
+    return CKV_OK;
+}
+
+ckv_status ckv_prefill_attention(const ckv_config* cfg, const ckv_batch* batch, const void* q,
+                                 int64_t q_tok_stride, int64_t q_head_stride, const void* k,
+                                 const void* v, int64_t tok_stride, int64_t head_stride, void* out,
+                                 float* lse, int64_t lse_head_stride, float* lse_win,
+                                 int64_t lse_win_head_stride, void* workspace, size_t workspace_bytes,
+                                 ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int T = 0;
+    AttnWs l;
+    if ((st = check_batch(batch, &T)) || (st = check_strides("q", cfg->num_q_heads, &q_tok_stride, &q_head_stride)) ||
+        (st = check_strides("k/v", cfg->num_kv_heads, &tok_stride, &head_stride)) || (st = check_kv(q, "q", T)) ||
+        (st = check_kv(k, "k", T)) || (st = check_kv(v, "v", T)) || (st = check_kv(out, "out", T)) ||
+        (st = check_lse_out("lse", lse, T, &lse_head_stride)) ||
+        (st = check_lse_out("lse_win", lse_win, static_cast<int64_t>(batch->num_seqs) * cfg->window,
+                            &lse_win_head_stride)) ||
+        (st = check_attn_ws(workspace, workspace_bytes, &l)))
+        return st;
+    if (T == 0) return CKV_OK;
+    AttnLaunch L;
+    memset(&L, 0, sizeof L);
+    attn_common(L, cfg, workspace, l);
+    L.q = q;
+    L.q_tok = q_tok_stride;
+    L.q_head = q_head_stride;
+    L.k = k;
+    L.v = v;
+    L.tok_stride = tok_stride;
+    L.head_stride = head_stride;
+    L.cu = batch->cu_seqlens_dev;
+    L.S = batch->num_seqs;
+    L.T = T;
+    L.out = out;
+    L.lse = lse;
+    L.lse_stride = lse_head_stride;
+    L.lse_win = lse_win;
+    L.lse_win_stride = lse_win_head_stride;
+    L.check_hash = true;
+    L.cu_hash = seqlens_hash(batch->cu_seqlens_host, batch->num_seqs);
+    return enqueue_attention(L, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ckv_status ckv_paged_attention(const ckv_config* cfg, const ckv_paged_cache* cache, int32_t num_seqs,
+                               int32_t num_tokens, const int32_t* block_table, int32_t max_blocks,
+                               const int32_t* cache_lens, const int32_t* cu_new, const void* q,
+                               int64_t q_tok_stride, int64_t q_head_stride, void* out, float* lse,
+                               int64_t lse_head_stride, void* workspace, size_t workspace_bytes,
+                               ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int64_t page_stride = 0;
+    AttnWs l;
+    if ((st = check_cache(cache, &page_stride)) || (st = resolve_page_stride(cache, cfg->num_kv_heads, &page_stride)))
+        return st;
+    if (num_seqs < 1) return fail(CKV_ERR_INVALID_ARG, "num_seqs %d < 1", num_seqs);
+    if (num_tokens < 0) return fail(CKV_ERR_INVALID_ARG, "num_tokens %d < 0", num_tokens);
+    if (max_blocks < 1) return fail(CKV_ERR_INVALID_ARG, "max_blocks %d < 1", max_blocks);
+    if (static_cast<int64_t>(max_blocks) * cache->page_size > INT_MAX - 128)
+        return fail(CKV_ERR_UNSUPPORTED, "block-table rows of more than 2^31 - 129 tokens");
+    if (!block_table || !cache_lens || !cu_new)
+        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens and cu_new are required");
+    if (!aligned(block_table, 4) || !aligned(cache_lens, 4) || !aligned(cu_new, 4))
+        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens or cu_new is not 4-byte aligned");
+    if ((st = check_strides("q", cfg->num_q_heads, &q_tok_stride, &q_head_stride)) ||
+        (st = check_kv(q, "q", num_tokens)) || (st = check_kv(out, "out", num_tokens)) ||
+        (st = check_lse_out("lse", lse, num_tokens, &lse_head_stride)) ||
+        (st = check_attn_ws(workspace, workspace_bytes, &l)))
+        return st;
+    if (num_tokens == 0) return CKV_OK;
+    AttnLaunch L;
+    memset(&L, 0, sizeof L);
+    attn_common(L, cfg, workspace, l);
+    L.q = q;
+    L.q_tok = q_tok_stride;
+    L.q_head = q_head_stride;
+    L.k = cache->k_pages;
+    L.v = cache->v_pages;
+    L.tok_stride = static_cast<int64_t>(cfg->num_kv_heads) * kHeadDim;
+    L.head_stride = kHeadDim;
+    L.cu = cu_new;
+    L.lens = cache_lens;
+    L.paged = true;
+    L.page_stride = page_stride;
+    L.page_size = cache->page_size;
+    L.num_pages = cache->num_pages;
+    L.max_blocks = max_blocks;
+    L.table = block_table;
+    L.S = num_seqs;
+    L.T = num_tokens;
+    L.out = out;
+    L.lse = lse;
+    L.lse_stride = lse_head_stride;
+    return enqueue_attention(L, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* cache_lens,
+                            const int32_t* new_lens, int32_t* free_pages, int32_t num_pages,
+                            const int64_t* pool, int32_t* block_table, int32_t max_blocks,
+                            int32_t* slot_map, int32_t num_slots, int32_t* cu_new, int32_t* lens_out,
+                            int64_t* pool_out, void* workspace, size_t workspace_bytes, ckv_stream stream) {
+    if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128)
+        return fail(page_size < 1 ? CKV_ERR_INVALID_ARG : CKV_ERR_UNSUPPORTED, "page_size %d (16, 32, 64 or 128)",
+                    page_size);
+    if (num_rows < 1) return fail(CKV_ERR_INVALID_ARG, "num_rows %d < 1", num_rows);
+    if (num_pages < 1) return fail(CKV_ERR_INVALID_ARG, "num_pages %d < 1", num_pages);
+    if (max_blocks < 1) return fail(CKV_ERR_INVALID_ARG, "max_blocks %d < 1", max_blocks);
+    if (num_slots < 0) return fail(CKV_ERR_INVALID_ARG, "num_slots %d < 0", num_slots);
+    if (static_cast<int64_t>(num_pages) * page_size > INT_MAX - 128 ||
+        static_cast<int64_t>(max_blocks) * page_size > INT_MAX - 128)
+        return fail(CKV_ERR_UNSUPPORTED, "more than 2^31 - 129 slots, or tokens of a row");
+    if (!cache_lens || !new_lens || !free_pages || !pool || !block_table || (!slot_map && num_slots > 0) || !cu_new ||
+        !lens_out || !pool_out)
+        return fail(CKV_ERR_INVALID_ARG, "every array is required");
+    for (const void* p : {static_cast<const void*>(cache_lens), static_cast<const void*>(new_lens),
+                          static_cast<const void*>(free_pages), static_cast<const void*>(block_table),
+                          static_cast<const void*>(slot_map), static_cast<const void*>(cu_new),
+                          static_cast<const void*>(lens_out)})
+        if (!aligned(p, 4)) return fail(CKV_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
+    if (!aligned(pool, 8) || !aligned(pool_out, 8))
+        return fail(CKV_ERR_INVALID_ARG, "pool or pool_out is not 8-byte aligned");
+    AttnWs l;
+    ckv_status st = check_attn_ws(workspace, workspace_bytes, &l);
+    if (st) return st;
+    TablesLaunch L;
+    L.page_size = page_size;
+    L.n_rows = num_rows;
+    L.num_pages = num_pages;
+    L.max_blocks = max_blocks;
+    L.cap = num_slots;
+    L.lens = cache_lens;
+    L.new_lens = new_lens;
+    L.free_pages = free_pages;
+    L.pool = reinterpret_cast<const long long*>(pool);
+    L.table = block_table;
+    L.slots = slot_map;
+    L.cu = cu_new;
+    L.lens_out = lens_out;
+    L.pool_out = reinterpret_cast<long long*>(pool_out);
+    L.status = static_cast<int*>(workspace);
+    L.ticket = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + l.ticket);
+    const cudaError_t e = launch_block_tables(L, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the block-table kernel");
+}
+
+ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache* cache, int32_t num_tokens,
+                           const void* k, const void* v, int64_t tok_stride, int64_t head_stride,
+                           const int32_t* slot_map, void* workspace, size_t workspace_bytes,
+                           ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int64_t page_stride = 0;
+    AttnWs l;
+    if ((st = check_cache(cache, &page_stride)) || (st = resolve_page_stride(cache, cfg->num_kv_heads, &page_stride)))
+        return st;
+    if (num_tokens < 0) return fail(CKV_ERR_INVALID_ARG, "num_tokens %d < 0", num_tokens);
+    if ((st = check_strides("k/v", cfg->num_kv_heads, &tok_stride, &head_stride)) ||
+        (st = check_kv(k, "k", num_tokens)) || (st = check_kv(v, "v", num_tokens)) ||
+        (st = check_attn_ws(workspace, workspace_bytes, &l)))
+        return st;
+    if (num_tokens == 0) return CKV_OK;
+    if (!slot_map || !aligned(slot_map, 4))
+        return fail(CKV_ERR_INVALID_ARG, "slot_map is required, 4-byte aligned");
+    CacheWriteLaunch L;
+    L.k = k;
+    L.v = v;
+    L.tok_stride = tok_stride;
+    L.head_stride = head_stride;
+    L.slots = slot_map;
+    L.k_pages = cache->k_pages;
+    L.v_pages = cache->v_pages;
+    L.page_stride = page_stride;
+    L.T = num_tokens;
+    L.Hkv = cfg->num_kv_heads;
+    L.shift = 0;
+    while ((1 << L.shift) < cache->page_size) ++L.shift;
+    L.num_slots = cache->num_pages * cache->page_size;
+    L.status = static_cast<int*>(workspace);
+    const cudaError_t e = launch_cache_write(L, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the cache-write kernel");
+}
+
 // The items per unit of a multi-layer launch, for the tests (host only; not part of the ABI): sequence s
 // of tiles[s] key tiles is cut into items[s] of them.
 __attribute__((visibility("default"))) int32_t ckv_internal_plan_items(

@@ -25,6 +25,7 @@ enum DeviceCode : int {
     kDevTimeout = 2,     // a bounded wait gave up
     kDevBadIndex = 3,    // an index read from device memory was out of range
     kDevRange = 4,       // a window row's largest logit is beyond the supported range
+    kDevPool = 5,        // the page pool, a table row or the slot map cannot hold the new tokens
 };
 
 // Workspace header: status code, detail, then padding to 256 bytes.

@@ -207,6 +207,67 @@ struct SrsLaunch {
 cudaError_t launch_srs_mask(const SrsLaunch& L, cudaStream_t stream);
 cudaError_t launch_srs_span(const SrsLaunch& L, cudaStream_t stream);
 
+// Causal attention (attention.cu): packed prompts, or new tokens over a paged cache.
+constexpr int kAttnMaxCtas = 160;   // CTAs of one launch, and the partial results the workspace holds
+constexpr int kAttnUnitRows = 256;  // query rows (of all heads of a unit) of one CTA, at most
+struct AttnLaunch {
+    const void* q;
+    int64_t q_tok, q_head;          // strides in elements
+    const void* k;                  // packed [T, H_kv, 128] by the strides below, or the cache's pages
+    const void* v;
+    int64_t tok_stride, head_stride;
+    const int32_t* cu;              // device [S+1]: query rows of each sequence, from cu[0]
+    const int32_t* lens;            // device [S]: keys of each sequence (null: its query rows)
+    bool paged;
+    int64_t page_stride;            // elements between pages; a page is [page_size, H_kv, 128]
+    int page_size, num_pages, max_blocks;
+    const int32_t* table;           // device [S][max_blocks]
+    int S, T, Hq, Hkv, w, max_ctas;
+    float scale;
+    void* out;                      // [T, H_q, 128]
+    float* lse;                     // [H_q][lse_stride], or null
+    int64_t lse_stride;
+    float* lse_win;                 // [H_q][lse_win_stride], the last w rows of each sequence, or null
+    int64_t lse_win_stride;
+    int* status;
+    int* counters;                  // [kAttnMaxCtas], zero between calls
+    float* partials;                // [kAttnMaxCtas * 2][attn_partial_floats()]
+    bool check_hash;                // cu has to hash to cu_hash
+    uint32_t cu_hash;
+};
+// A partial result: an unnormalised output row, its reference maximum and its sum, per unit row.
+constexpr size_t attn_partial_floats() { return static_cast<size_t>(kAttnUnitRows) * (128 + 2); }
+cudaError_t launch_attention(const AttnLaunch& L, cudaStream_t stream);
+
+// The paged cache (paged_cache.cu).
+struct TablesLaunch {
+    int page_size, n_rows, num_pages, max_blocks, cap;
+    const int32_t* lens;
+    const int32_t* new_lens;
+    int32_t* free_pages;            // ring of num_pages entries
+    const long long* pool;          // {pages ever taken, pages ever returned}
+    int32_t* table;
+    int32_t* slots;
+    int32_t* cu;
+    int32_t* lens_out;
+    long long* pool_out;
+    int* status;
+    int* ticket;                    // zero between calls
+};
+cudaError_t launch_block_tables(const TablesLaunch& L, cudaStream_t stream);
+struct CacheWriteLaunch {
+    const void* k;
+    const void* v;
+    int64_t tok_stride, head_stride;
+    const int32_t* slots;           // [T], -1: skipped
+    void* k_pages;
+    void* v_pages;
+    int64_t page_stride;
+    int T, Hkv, shift, num_slots;
+    int* status;
+};
+cudaError_t launch_cache_write(const CacheWriteLaunch& L, cudaStream_t stream);
+
 int device_sm_count();
 
 }  // namespace ckv
