@@ -416,7 +416,9 @@ CKV_API ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer,
  * softmax's numerators are rounded to bf16 for the product with v, as the outputs are at the end.
  * Logits are below 1e8 in magnitude.  v is finite: a NaN or an infinity in a value row can reach query
  * rows of its sequence that stand less than 256 tokens before it, never another sequence.  What a query
- * row does not see of k may be anything. */
+ * row does not see of k may be anything.  How a sequence's keys are split over CTAs depends on the
+ * call's other sequences and on max_ctas, so the same sequence's results can differ in their last bits
+ * from call to call; the same call gives the same bits. */
 
 CKV_API ckv_status ckv_attention_workspace_size(const ckv_config* cfg, size_t* bytes);
 

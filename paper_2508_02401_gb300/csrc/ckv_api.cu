@@ -1681,8 +1681,54 @@ ckv_status resolve_page_stride(const ckv_paged_cache* c, int Hkv, int64_t* page_
     return CKV_OK;
 }
 
+// A bf16 tensor of `rank` dimensions, {128, ...}, 128-byte swizzled like the MMA operands; strides in
+// elements, the innermost being 1.
+ckv_status make_rows_map(CUtensorMap* map, const void* ptr, int rank, const int64_t* dims, const int64_t* strides,
+                         const int* box) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return fail(CKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+    cuuint64_t d[4], st[3];
+    cuuint32_t b[4];
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        d[i] = static_cast<cuuint64_t>(dims[i]);
+        b[i] = static_cast<cuuint32_t>(box[i]);
+        if (i > 0) st[i - 1] = static_cast<cuuint64_t>(strides[i]) * 2;
+    }
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), d, st, b, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(CKV_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+    return CKV_OK;
+}
+
 ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
-    const cudaError_t e = launch_attention(L, stream);
+    const int hp = attn_heads_per_tile(L.Hq, L.Hkv), tp = kTileKeys / hp;
+    // Two row tiles a unit where the sequences have more rows than one tile on average.
+    const int tiles = static_cast<int64_t>(L.T) > static_cast<int64_t>(L.S) * tp ? 2 : 1;
+    CUtensorMap mq, mk, mv;
+    ckv_status st;
+    {
+        const int64_t dims[3] = {kHeadDim, L.Hq, L.T}, strides[3] = {1, L.q_head, L.q_tok};
+        const int box[3] = {64, hp, tp};
+        if ((st = make_rows_map(&mq, L.q, 3, dims, strides, box))) return st;
+    }
+    for (int i = 0; i < 2; ++i) {
+        const void* ptr = i ? L.v : L.k;
+        CUtensorMap* map = i ? &mv : &mk;
+        if (L.paged) {
+            const int64_t dims[4] = {kHeadDim, L.Hkv, L.page_size, L.num_pages};
+            const int64_t strides[4] = {1, L.head_stride, L.tok_stride, L.page_stride};
+            const int box[4] = {64, 1, L.page_size, 1};
+            st = make_rows_map(map, ptr, 4, dims, strides, box);
+        } else {
+            const int64_t dims[3] = {kHeadDim, L.Hkv, L.T}, strides[3] = {1, L.head_stride, L.tok_stride};
+            const int box[3] = {64, 1, kTileKeys};
+            st = make_rows_map(map, ptr, 3, dims, strides, box);
+        }
+        if (st) return st;
+    }
+    const cudaError_t e = launch_attention(L, mq, mk, mv, tiles, stream);
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 

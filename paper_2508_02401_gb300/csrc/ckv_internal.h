@@ -237,7 +237,10 @@ struct AttnLaunch {
 };
 // A partial result: an unnormalised output row, its reference maximum and its sum, per unit row.
 constexpr size_t attn_partial_floats() { return static_cast<size_t>(kAttnUnitRows) * (128 + 2); }
-cudaError_t launch_attention(const AttnLaunch& L, cudaStream_t stream);
+// Query heads of a KV group that share a tile of 128 (token, head) rows.
+constexpr int attn_heads_per_tile(int Hq, int Hkv) { return Hq / Hkv < 128 ? Hq / Hkv : 128; }
+cudaError_t launch_attention(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
+                             const CUtensorMap& map_v, int tiles, cudaStream_t stream);
 
 // The paged cache (paged_cache.cu).
 struct TablesLaunch {

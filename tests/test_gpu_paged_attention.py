@@ -196,7 +196,7 @@ def test_same_results_on_another_stream_and_again():
 def test_bad_lengths_and_pages_are_reported(what):
     """Other sequences' rows are right all the same; nothing outside the outputs is touched."""
     c = Paged(config(8, 2), (300, 200, 400), (1, 3, 2), 32, seed=14)
-    want = c.run()[0].clone()
+    lens = list(c.lens)
     good = [0, 2]
     if what == "page":
         c.table[1, 3] = c.k_pages.shape[0]
@@ -214,9 +214,11 @@ def test_bad_lengths_and_pages_are_reported(what):
     out, lse = c.run(status=(3, 0))
     if not good:
         assert bool((out == 7).all()) and bool((lse == 7).all())
-    for s in good:
+    for s in good:  # (how a sequence is cut over CTAs, and so its last bits, depends on the others)
         a, b = rows[s]
-        assert torch.equal(out[a:b], want[a:b])
+        o, l, tol, tol_l = ref.rows(c.q[a:b], c.k[s], c.v[s], torch.arange(lens[s] - (b - a), lens[s]))
+        ref.assert_close(out[a:b], o, tol, f"out of sequence {s}")
+        ref.assert_close(lse[:, a:b], l, tol_l, f"lse of sequence {s}")
 
 
 def test_refusals():
