@@ -29,6 +29,8 @@ constexpr int kAttnItemRing = 4;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kQWarp = 10;  // warps 0-3, 4-7: softmax; 10, 11: query rows
 // A row's reference moves when a tile's maximum passes it by 2^8.
 constexpr float kAttnTau = 8.0f;
+// What a unit costs beside its key tiles, in key tiles: its first ones stand before its tiles in a run.
+constexpr int kUnitCost = 3;
 
 struct alignas(128) AttnParams {
     CUtensorMap tmap_q;  // {128, H_q, T}, box {64, hp, tp}   (TILES = 2)
@@ -177,14 +179,15 @@ __device__ __forceinline__ Seq get_seq(const AttnLaunch& a, int s, int cu0, bool
     return q;
 }
 
-// Key tiles of row tile j of a sequence, and of the tiles before it (j = nj: of all nj).
+// Key tiles of row tile j of a sequence, and the cost of the row tiles before it (j = nj: of all nj), in key
+// tiles and kUnitCost for each.
 __device__ __forceinline__ int unit_tiles(const Seq& q, int tq, int j) {
     return (q.len - q.n + min((j + 1) * static_cast<long long>(tq), static_cast<long long>(q.n)) - 1) / kTileKeys + 1;
 }
-__device__ __forceinline__ long long tiles_before(const Seq& q, int tq, int j, int nj) {
+__device__ __forceinline__ long long cost_before(const Seq& q, int tq, int j, int nj) {
     const int full = j == nj ? nj - 1 : j;
-    long long s = 0;
-    if (full > 0) s = static_cast<long long>(floor_sum(full, kTileKeys, tq, q.len - q.n + tq - 1)) + full;
+    long long s = static_cast<long long>(j) * kUnitCost;
+    if (full > 0) s += static_cast<long long>(floor_sum(full, kTileKeys, tq, q.len - q.n + tq - 1)) + full;
     return j == nj && nj > 0 ? s + unit_tiles(q, tq, nj - 1) : s;
 }
 
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
         return;
     }
 
-    // ---- this CTA's run: key tiles [w0, w1) of all units' in order
+    // ---- this CTA's run: positions [w0, w1) of all units' in order, a unit's being kUnitCost and its tiles
     const int cu0 = a.cu[0];
     const int per = (a.S + kAttnThreads - 1) / kAttnThreads;
     const int s_lo = min(static_cast<long long>(threadIdx.x) * per, static_cast<long long>(a.S));
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
     for (int s = s_lo; s < s_hi; ++s) {
         const Seq q = get_seq(a, s, cu0, bad, blockIdx.x == 0);
         const int nj = (q.n + tq - 1) / tq;
-        if (q.n > 0) own += tiles_before(q, tq, nj, nj);
+        if (q.n > 0) own += cost_before(q, tq, nj, nj);
     }
     own *= heads;
     long long incl = own;
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
             bool b = false;
             const Seq q = get_seq(a, s, cu0, b, false);
             const int nj = (q.n + tq - 1) / tq;
-            const long long w = q.n > 0 ? heads * tiles_before(q, tq, nj, nj) : 0;
+            const long long w = q.n > 0 ? heads * cost_before(q, tq, nj, nj) : 0;
             if (w0 < at + w) {
                 scan[13] = s;
                 scan[14] = w0 - at;
@@ -340,16 +343,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
                 int lo = 0, hi = nj;
                 while (hi - lo > 1) {
                     const int step = (hi - lo + 31) / 32, cand = lo + lane * step;
-                    const bool le = cand < hi && heads * tiles_before(q, tq, cand, nj) <= off;
+                    const bool le = cand < hi && heads * cost_before(q, tq, cand, nj) <= off;
                     const int top = 31 - __clz(__ballot_sync(0xffffffffu, le));
                     lo += top * step;
                     hi = min(hi, lo + step);
                 }
                 j = lo;
-                off -= heads * tiles_before(q, tq, j, nj);
-                const int kt = unit_tiles(q, tq, j);
-                hb = static_cast<int>(off / kt);
-                t0 = static_cast<int>(off - static_cast<long long>(hb) * kt);
+                off -= heads * cost_before(q, tq, j, nj);
+                const int cost = unit_tiles(q, tq, j) + kUnitCost;
+                hb = static_cast<int>(off / cost);
+                t0 = static_cast<int>(off - static_cast<long long>(hb) * cost);
+                at += max(0, kUnitCost - t0);  // the position of tile t0
+                t0 = max(0, t0 - kUnitCost);
             }
             uint32_t use = 0, qn[2] = {0, 0};
             int it = 0;
@@ -384,7 +389,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
                     I.part = -1;
                     I.n_parts = 1;
                     I.cta0 = 0;
-                    if (t0 > 0 || t1 < kt) {  // the CTA of flat tile x is floor(((x + 1) ctas - 1) / W)
+                    if (t0 > 0 || t1 < kt) {  // the CTA of position x is floor(((x + 1) ctas - 1) / W)
                         const long long u0 = at - t0;
                         I.cta0 = static_cast<int>(((u0 + 1) * ctas - 1) / W);
                         I.n_parts = static_cast<int>(((u0 + kt) * ctas - 1) / W) - I.cta0 + 1;
@@ -476,7 +481,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
                     ok = ok && load(&p.tmap_v, u);
                 }
                 // the next unit
-                at += I.n_tiles;
+                at += I.n_tiles + kUnitCost;
                 t0 = 0;
                 if (++hb == heads) {
                     hb = 0;
@@ -845,53 +850,85 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(const __grid
                 }
                 if (!(ok = pair_sync(pair, pair_phase, abort, lim))) break;
                 if (*verdict) {
-                    // this CTA finished last: join the parts, four columns of a row at a time
+                    // this CTA finished last: join the parts
                     __threadfence();
-                    int rows = kRows, shift = TILES == 2 ? 8 : 7;
-                    if (TILES == 1) {
-                        const int used = I.ntok * p.hp;
-                        shift = used <= 1 ? 0 : 32 - __clz(used - 1);
-                        rows = 1 << shift;
-                    }
-                    for (int e = threadIdx.x; e < 32 * rows; e += 256) {
-                        const int rr = e & (rows - 1), c4 = e >> shift;
-                        const int rx = rr & 127, ti = rx / p.hp, hi = rx - ti * p.hp;
-                        const int tk = ti + (TILES == 2 ? (rr >> 7) * p.tp : 0);
-                        if (ti >= p.tp || tk >= I.ntok || hi >= I.nheads) continue;
-                        float M = -INFINITY, L = 0.f;
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int k0 = 0; k0 < I.n_parts; k0 += 4) {
-                            float pm[4], pl[4];
-                            float4 po[4];
+                    auto part_of = [&](int k) {
+                        return a.partials + (static_cast<size_t>(I.cta0 + k) * 2 + (k == 0 ? 1 : 0)) * attn_partial_floats();
+                    };
+                    if (TILES == 1 && I.ntok * p.hp <= 16) {
+                        // few rows, perhaps many parts: four columns of a row a thread, four parts at a time
+                        for (int e = threadIdx.x; e < 32 * 16; e += 256) {
+                            const int rr = e & 15, c4 = e >> 4;
+                            const int ti = rr / p.hp, hi = rr - ti * p.hp;
+                            if (ti >= I.ntok || hi >= I.nheads) continue;
+                            float M = -INFINITY, L = 0.f;
+                            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                            for (int k0 = 0; k0 < I.n_parts; k0 += 4) {
+                                float pm[4], pl[4];
+                                float4 po[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                pm[k] = -INFINITY;
-                                if (k0 + k >= I.n_parts) continue;
-                                const float* src = a.partials + (static_cast<size_t>(I.cta0 + k0 + k) * 2 + (k0 + k == 0 ? 1 : 0)) *
-                                                                    attn_partial_floats();
-                                pm[k] = __ldcg(src + kRows * 128 + rr);
-                                pl[k] = __ldcg(src + kRows * 129 + rr);
-                                po[k] = __ldcg(reinterpret_cast<const float4*>(src) + c4 * kRows + rr);
+                                for (int k = 0; k < 4; ++k) {
+                                    pm[k] = -INFINITY;
+                                    if (k0 + k >= I.n_parts) continue;
+                                    const float* src = part_of(k0 + k);
+                                    pm[k] = __ldcg(src + kRows * 128 + rr);
+                                    pl[k] = __ldcg(src + kRows * 129 + rr);
+                                    po[k] = __ldcg(reinterpret_cast<const float4*>(src) + c4 * kRows + rr);
+                                }
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    if (pm[k] == -INFINITY) continue;  // no key seen: its values are not to be used
+                                    const float Mn = fmaxf(M, pm[k]);
+                                    const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn), f1 = ex2_approx(pm[k] - Mn);
+                                    M = Mn;
+                                    L = L * f0 + pl[k] * f1;
+                                    acc.x = acc.x * f0 + po[k].x * f1;
+                                    acc.y = acc.y * f0 + po[k].y * f1;
+                                    acc.z = acc.z * f0 + po[k].z * f1;
+                                    acc.w = acc.w * f0 + po[k].w * f1;
+                                }
                             }
+                            const float inv = 1.f / L;
+                            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
+                                                 (static_cast<long long>(I.q_row + ti) * a.Hq + I.head0 + hi) * kHeadDim + c4 * 4;
+                            *reinterpret_cast<uint2*>(out) =
+                                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                            if (c4 == 0) write_lse(ti, hi, M, L);
+                        }
+                    } else if (valid) {  // a thread its row (half of it), part after part
+                        float acc[kCols], M = -INFINITY, L = 0.f;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if (pm[k] == -INFINITY) continue;  // (its values were not written)
-                                const float Mn = fmaxf(M, pm[k]);
-                                const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn), f1 = ex2_approx(pm[k] - Mn);
-                                M = Mn;
-                                L = L * f0 + pl[k] * f1;
-                                acc.x = acc.x * f0 + po[k].x * f1;
-                                acc.y = acc.y * f0 + po[k].y * f1;
-                                acc.z = acc.z * f0 + po[k].z * f1;
-                                acc.w = acc.w * f0 + po[k].w * f1;
+                        for (int x = 0; x < kCols; ++x) acc[x] = 0.f;
+#pragma unroll 1
+                        for (int k = 0; k < I.n_parts; ++k) {
+                            const float* src = part_of(k);
+                            const float pm = __ldcg(src + kRows * 128 + row), pl = __ldcg(src + kRows * 129 + row);
+                            float4 po[kCols / 4];
+#pragma unroll
+                            for (int x = 0; x < kCols / 4; ++x)
+                                po[x] = __ldcg(reinterpret_cast<const float4*>(src) + ((col0 >> 2) + x) * kRows + row);
+                            if (pm == -INFINITY) continue;  // no key seen: its values are not to be used
+                            const float Mn = fmaxf(M, pm);
+                            const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn), f1 = ex2_approx(pm - Mn);
+                            M = Mn;
+                            L = L * f0 + pl * f1;
+#pragma unroll
+                            for (int x = 0; x < kCols / 4; ++x) {
+                                acc[4 * x] = acc[4 * x] * f0 + po[x].x * f1;
+                                acc[4 * x + 1] = acc[4 * x + 1] * f0 + po[x].y * f1;
+                                acc[4 * x + 2] = acc[4 * x + 2] * f0 + po[x].z * f1;
+                                acc[4 * x + 3] = acc[4 * x + 3] * f0 + po[x].w * f1;
                             }
                         }
                         const float inv = 1.f / L;
                         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
-                                             (static_cast<long long>(I.q_row + tk) * a.Hq + I.head0 + hi) * kHeadDim + c4 * 4;
-                        *reinterpret_cast<uint2*>(out) =
-                            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                        if (c4 == 0) write_lse(tk, hi, M, L);
+                                             (static_cast<long long>(I.q_row + tok) * a.Hq + I.head0 + h_r) * kHeadDim + col0;
+#pragma unroll
+                        for (int x = 0; x < kCols; x += 8)
+                            *reinterpret_cast<uint4*>(out + x) =
+                                make_uint4(pack_bf16(acc[x] * inv, acc[x + 1] * inv), pack_bf16(acc[x + 2] * inv, acc[x + 3] * inv),
+                                           pack_bf16(acc[x + 4] * inv, acc[x + 5] * inv), pack_bf16(acc[x + 6] * inv, acc[x + 7] * inv));
+                        if (col0 == 0) write_lse(tok, h_r, M, L);
                     }
                 }
             }
