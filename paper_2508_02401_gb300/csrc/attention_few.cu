@@ -1,0 +1,530 @@
+// Attention of a few query rows a sequence over a paged cache (attention_common.cuh): single tokens, short drafts.
+//
+// With G heads of one token on a KV head, 128 rows of the MMA would hold G; so the keys take the MMA's M and the
+// N (token, head) rows its N: S^T [128 keys][N] = K Q^T, a key a thread, and O^T [128 dims][N] += V^T P with the
+// numerators P [128 keys][N] in shared memory.  Every thread has N exponentials a tile, the rows' sums stay in the
+// threads until a unit's end, and the reference of a row is moved by the warps together when a vote says so.
+//
+// Bound by the loads of K and V: 64 KB a key tile, 1.5 us of an SM's share of the bandwidth, against some 0.6 us of
+// the path K tile - logits - numerators - product.  With N = 16 two CTAs run on an SM, so that one's start and end
+// of a unit lie beside the other's loads.
+#include "attention_common.cuh"
+
+namespace ckv {
+namespace {
+
+constexpr int kThreadsF = 256;
+constexpr int kMmaWarpF = 4, kLoadWarpF = 5, kQWarpF = 6;  // warps 0-3: softmax; 7: idle
+
+template <int N>
+struct FewCfg {
+    static constexpr int kCtas = N == 16 ? 2 : 1;                  // on an SM
+    static constexpr int kRing = N == 16 ? 3 : (N == 32 ? 6 : 5);  // K and V tiles of 32 KB
+    static constexpr int kQBytes = N * 256;                        // two buffers
+    static constexpr int kPBytes = N * 256;
+    static constexpr int kTmem = N == 16 ? 64 : 4 * N;             // columns: two S, one O
+    // P as the MMA's B: rows of 2 N bytes a key, swizzled over as many bytes; 8-key groups
+    static constexpr uint32_t kPGroup = 16 * N;
+    static constexpr uint32_t kPHi = (kPGroup >> 4) | (1u << 14) | ((N == 16 ? 6u : (N == 32 ? 4u : 2u)) << 29);
+    static constexpr int kQ = kRing * kTileBytes;
+    static constexpr int kP = kQ + 2 * kQBytes;
+    static constexpr int kRed = kP + kPBytes;   // float [4][N]
+    static constexpr int kRef = kRed + 16 * N;  // float [N]: the rows' references, times c
+    static constexpr int kItems = kRef + 4 * N;
+    static constexpr int kBars = kItems + kAttnItemRing * static_cast<int>(sizeof(Item));
+    static constexpr int kFull = 0, kFree = kFull + kRing, kQFull = kFree + kRing, kQFree = kQFull + 2,
+                         kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 1, kItemFull = kPvDone + 1,
+                         kItemFree = kItemFull + kAttnItemRing, kDone = kItemFree + kAttnItemRing, kNumBars = kDone + 1;
+    static constexpr int kScan = kBars + 8 * ((kNumBars + 1) & ~1);
+    static constexpr int kMisc = kScan + 8 * 16;
+    static constexpr int kBytes = kMisc + 16;
+    static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * N * 130 <= kAttnPartialFloats, "workspace");
+    static_assert(kBytes <= (kCtas == 2 ? 115712 : 232448), "shared memory");
+};
+
+// Barriers of the softmax warps.  None leaves without the others: they agree on every item, and no wait for a
+// tile makes one leave.
+__device__ __forceinline__ void group_bar() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool group_or(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(x ? 1u : 0u)
+        : "memory");
+    return r != 0;
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_ldn(uint32_t taddr, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 16) tmem_ld16_nowait(taddr + i, reinterpret_cast<float(&)[16]>(v[i]));
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < N; i += 16) reg_fence(reinterpret_cast<float(&)[16]>(v[i]));
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_kernel(const __grid_constant__ AttnParams p) {
+    using C = FewCfg<N>;
+    constexpr uint32_t kIdescS = idesc_bf16_f32(128, N);
+    constexpr uint32_t kIdescO = idesc_bf16_f32(128, N) | (1u << 15) | (1u << 16);  // A and B with M, N contiguous
+    extern __shared__ __align__(1024) uint8_t sm[];
+    uint8_t* ring = sm;
+    uint8_t* qbuf = sm + C::kQ;
+    uint8_t* pbuf = sm + C::kP;
+    float* red = reinterpret_cast<float*>(sm + C::kRed);
+    float* ref = reinterpret_cast<float*>(sm + C::kRef);
+    Item* items = reinterpret_cast<Item*>(sm + C::kItems);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sm + C::kBars);
+    uint64_t* full = bars + C::kFull;
+    uint64_t* freed = bars + C::kFree;
+    uint64_t* q_full = bars + C::kQFull;
+    uint64_t* q_free = bars + C::kQFree;
+    uint64_t* s_full = bars + C::kSFull;
+    uint64_t* p_full = bars + C::kPFull;
+    uint64_t* pv_done = bars + C::kPvDone;
+    uint64_t* item_full = bars + C::kItemFull;
+    uint64_t* item_free = bars + C::kItemFree;
+    uint64_t* done = bars + C::kDone;
+    long long* scan = reinterpret_cast<long long*>(sm + C::kScan);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + C::kMisc);
+    volatile int* abort = reinterpret_cast<volatile int*>(sm + C::kMisc + 4);
+    volatile int* verdict = reinterpret_cast<volatile int*>(sm + C::kMisc + 8);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const AttnLaunch& a = p.a;
+    const int heads = a.Hkv * p.nhb;    // units of a row tile
+    if ((smem_u32(sm) & 1023u) != 0) {  // the swizzled tiles need an aligned base
+        if (threadIdx.x == 0) record_error(a.status, kDevBadIndex, -2);
+        return;
+    }
+    if (threadIdx.x == 0) *abort = 0;
+    Run run;
+    if (!find_run<kThreadsF>(p, p.tp, heads, scan, run)) return;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::kRing; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&freed[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_free[i], 1);
+            mbar_init(&s_full[i], 1);
+        }
+        mbar_init(p_full, 4);
+        mbar_init(pv_done, 1);
+        for (int i = 0; i < kAttnItemRing; ++i) {
+            mbar_init(&item_full[i], 1);
+            mbar_init(&item_free[i], 6);  // softmax warps, the MMA issuer, the query loader
+        }
+        mbar_init(done, 1);
+        fence_mbar_init();
+    }
+    if (warp == kLoadWarpF && lane == 0) {
+        tma_prefetch_desc(&p.tmap_k);
+        tma_prefetch_desc(&p.tmap_v);
+    }
+    if (warp == kMmaWarpF) {
+        tmem_alloc(tmem_slot, C::kTmem);
+        tmem_relinquish();
+    }
+    // Query rows that a unit does not have are never loaded: zeros (or another unit's rows) in their place.
+    for (int i = threadIdx.x; i < 2 * C::kQBytes / 16; i += kThreadsF) reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tm_s = *tmem_slot, tm_o = tm_s + 2 * N;  // S of even and odd tiles, O
+    const long long lim = p.wait_cycles;
+
+    if (warp == kLoadWarpF) {
+        // ---------------------------------------------------------------- items, K and V tiles
+        Walk walk(p, run, p.tp, heads, scan);
+        TileLoader<true, C::kRing> tiles{p, ring, full, freed, abort, lim};
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing;
+            if (!(ok = warp_wait(&item_free[slot], ((it / kAttnItemRing) & 1) ^ 1, abort, lim))) break;
+            Item I;
+            const bool more = walk.next(I);
+            if (lane == 0) {
+                items[slot] = I;
+                mbar_arrive(&item_full[slot]);
+            }
+            __syncwarp();
+            if (!more) break;
+            ok = tiles.item(I);
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 51);
+            tiles.drain();
+        }
+        __syncwarp();
+    } else if (warp == kQWarpF) {
+        // ---------------------------------------------------------------- query rows
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing, qs = it & 1;
+            if (!(ok = warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim))) break;
+            const Item I = items[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&item_free[slot]);
+            if (I.part == kEndItem) break;
+            if (!(ok = warp_wait(&q_free[qs], ((it >> 1) & 1) ^ 1, abort, lim))) break;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
+            uint8_t* dst = qbuf + qs * C::kQBytes;
+            const int chunks = I.ntok * p.hp * 16;
+#pragma unroll 4
+            for (int x = lane; x < chunks; x += 32) {
+                const int r = x >> 4, ch = x & 15;
+                const int t = r / p.hp, h = r - t * p.hp;
+                if (h >= I.nheads) continue;
+                const uint4 val = *reinterpret_cast<const uint4*>(
+                    src + (I.q_row + t) * a.q_tok + (I.head0 + h) * a.q_head + ch * 8);
+                *reinterpret_cast<uint4*>(dst + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[qs]);
+            __syncwarp();
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 53);
+        }
+    } else if (warp == kMmaWarpF) {
+        // ---------------------------------------------------------------- MMA issuer
+        // The logits of a tile (of the next item's first) before the product of the one before it: S has two buffers,
+        // and the numerators of a tile are there only when its S has been read.
+        constexpr uint32_t kTileUnits = kTileBytes >> 4;
+        const uint32_t ring_addr = desc_addr(ring), q_addr = desc_addr(qbuf), p_lo = desc_addr(pbuf) | (1u << 16);
+        uint32_t sn = 0, pn = 0, cs = 0, cph = 0;  // logits and products issued; ring slot and phase of the next K
+        int it = 0, end_ = 0, n_ = 0, keys_ = 0;
+        bool ok = true;
+        auto fetch = [&]() {
+            const int slot = it % kAttnItemRing;
+            if (!warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim)) return false;
+            end_ = uniform(items[slot].part == kEndItem);
+            n_ = uniform(items[slot].n_tiles);
+            keys_ = uniform(items[slot].len - items[slot].t0 * kTileKeys);
+            __syncwarp();
+            if (elect_one()) mbar_arrive(&item_free[slot]);
+            __syncwarp();
+            ++it;
+            return true;
+        };
+        auto slot_of = [&](uint32_t d) { return cs + d >= C::kRing ? cs + d - C::kRing : cs + d; };
+        auto phase_of = [&](uint32_t d) { return cs + d >= C::kRing ? cph ^ 1 : cph; };
+        auto qk = [&](uint32_t d, bool first, bool last) {  // K at ring position d; item it - 1
+            const uint32_t ks = slot_of(d), qs = (it - 1) & 1;
+            if (first && !warp_wait(&q_full[qs], ((it - 1) >> 1) & 1, abort, lim)) return false;
+            const uint32_t k_lo = uniform((ring_addr + ks * kTileUnits) | kDescLoK);
+            const uint32_t q_lo = uniform((q_addr + qs * (C::kQBytes >> 4)) | kDescLoK);
+            const uint32_t d_tmem = uniform(tm_s + (sn & 1) * N);
+            tile_wait(&full[ks], phase_of(d), abort, lim, a.status);
+            __syncwarp();
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    umma_ss<kDescHi>(d_tmem, k_lo + (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2,
+                                     q_lo + (kk >> 2) * (N * 128 >> 4) + (kk & 3) * 2, kIdescS, kk > 0 ? 1u : 0u);
+                umma_commit(&s_full[sn & 1]);
+                umma_commit(&freed[ks]);
+                if (last) umma_commit(&q_free[qs]);
+            }
+            __syncwarp();
+            ++sn;
+            return true;
+        };
+        ok = fetch();
+        if (ok && !end_) ok = qk(0, true, n_ == 1);
+        while (ok && !end_) {
+            const int n = n_, keys = keys_;
+            for (int i = 0; i < n && ok; ++i) {
+                const bool last = i == n - 1;
+                if (last && !(ok = fetch())) break;
+                // ring: K(i) V(i) K(i + 1)
+                if (!last) ok = qk(2, false, i + 2 == n);
+                else if (!end_) ok = qk(2, true, n_ == 1);
+                if (!ok) break;
+                const uint32_t vs = slot_of(1);
+                const uint32_t v_lo = uniform((ring_addr + vs * kTileUnits) | kDescLoV), d_tmem = uniform(tm_o);
+                const uint32_t accumulate = uniform(i > 0);
+                tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
+                if (keys - i * kTileKeys < kTileKeys) clear_rows(ring + vs * kTileBytes, keys - i * kTileKeys, lane);
+                tile_wait(p_full, pn & 1, abort, lim, a.status);
+                ++pn;
+                __syncwarp();
+                tc_fence_after_sync();
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma_ss<C::kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * C::kPGroup >> 4), kIdescO,
+                                         kk > 0 ? 1u : accumulate);
+                    umma_commit(pv_done);
+                    umma_commit(&freed[vs]);
+                }
+                __syncwarp();
+                cph = phase_of(2);
+                cs = slot_of(2);
+            }
+        }
+        if (elect_one()) {
+            if (!ok) {
+                *abort = 1;
+                record_error(a.status, kDevTimeout, 52);
+            }
+            umma_commit(done);
+        }
+        __syncwarp();
+        volatile int never = 0;
+        mbar_wait(done, 0, &never);
+        __syncwarp();
+    } else if (warp < 4) {
+        // ---------------------------------------------------------------- softmax, a key a thread
+        const int key = threadIdx.x;
+        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+        const float c = p.c;
+        uint32_t sn = 0;
+        bool ok = true;
+        float l[N];  // this thread's keys' sums
+        // The product of the tile before the current one is in O, and its numerators have been read.
+        auto wait_pv = [&](uint32_t tile) {
+            if (tile == 0) return;
+            tile_wait(pv_done, (tile - 1) & 1, abort, lim, a.status);
+            __syncwarp();
+            tc_fence_after_sync();
+        };
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing;
+            ok = !group_or(!warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim));
+            if (!ok) break;
+            const Item I = items[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&item_free[slot]);
+            if (I.part == kEndItem) break;
+#pragma unroll
+            for (int x = 0; x < N; ++x) l[x] = 0.f;
+            if (key < N) ref[key] = -INFINITY;
+            group_bar();
+            const int rows = I.ntok * p.hp;
+            // The first key that some row does not see.
+            const int first_end = I.pos0 + 1;
+            for (int i = 0; i < I.n_tiles; ++i, ++sn) {
+                const int k0 = (I.t0 + i) * kTileKeys;
+                tile_wait(&s_full[sn & 1], (sn >> 1) & 1, abort, lim, a.status);
+                __syncwarp();
+                tc_fence_after_sync();
+                float s[N];
+                tmem_ldn<N>(tm_s + (sn & 1) * N + lane_base, s);
+                tc_fence_before_sync();
+                if (k0 + kTileKeys > first_end) {
+                    int ends = first_end - (k0 + key), h = 0;  // positive: the row of column x sees the key
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        s[x] = ends > 0 ? s[x] : -INFINITY;
+                        if (++h == p.hp) {
+                            h = 0;
+                            ++ends;
+                        }
+                    }
+                }
+                float over = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    s[x] *= c;
+                    over = fmaxf(over, x < rows ? s[x] - ref[x] : -INFINITY);
+                }
+                const bool moved = group_or(over > kAttnTau);
+                wait_pv(sn);
+                if (moved) {
+                    // Move the references that a key passes by more than 2^8 (or that have none yet).
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        const float w = redux_max(s[x]);
+                        if (lane == 0) red[warp * N + x] = w;
+                    }
+                    group_bar();
+#pragma unroll
+                    for (int x0 = 0; x0 < N; x0 += 16) {
+                        float o[16];
+                        if (i > 0) {
+                            tmem_ld16_nowait(tm_o + lane_base + x0, o);
+                            tmem_ld_wait();
+                            reg_fence(o);
+                        }
+#pragma unroll
+                        for (int x = x0; x < x0 + 16; ++x) {
+                            const float mx = fmaxf(fmaxf(red[x], red[N + x]), fmaxf(red[2 * N + x], red[3 * N + x]));
+                            // (false for -inf - -inf)
+                            const float f = mx - ref[x] > kAttnTau ? ex2_approx(ref[x] - mx) : 1.f;
+                            l[x] *= f;
+                            o[x - x0] *= f;
+                        }
+                        if (i > 0) tmem_st16(tm_o + lane_base + x0, o);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    group_bar();  // ref is read
+                    if (key < N) {
+                        const float mx = fmaxf(fmaxf(red[key], red[N + key]), fmaxf(red[2 * N + key], red[3 * N + key]));
+                        if (mx - ref[key] > kAttnTau) ref[key] = mx;
+                    }
+                    group_bar();
+                }
+                uint32_t pk[N / 2];
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
+                    s[x] = ex2_approx(s[x] - fmaxf(ref[x], -3e38f));  // (-inf: a row that has seen no key yet)
+                    l[x] += s[x];
+                }
+#pragma unroll
+                for (int x = 0; x < N; x += 2) pk[x >> 1] = pack_bf16(s[x], s[x + 1]);
+                // The key's row of P, its 16-byte pieces swizzled by the address bits above the row's.
+#pragma unroll
+                for (int x = 0; x < N / 8; ++x) {
+                    const int sw = N == 16 ? (key >> 2) & 1 : (N == 32 ? (key >> 1) & 3 : key & 7);
+                    *reinterpret_cast<uint4*>(pbuf + key * (2 * N) + ((x ^ sw) << 4)) =
+                        make_uint4(pk[4 * x], pk[4 * x + 1], pk[4 * x + 2], pk[4 * x + 3]);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+                __syncwarp();
+            }
+            // ---- the unit's (or this part's) result: the rows' sums over the threads, then a dim a thread
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                if (x >= rows) break;
+                const float w = warp_sum(l[x]);
+                if (lane == 0) red[warp * N + x] = w;
+            }
+            wait_pv(sn);
+            group_bar();
+            float o[N];
+            tmem_ldn<N>(tm_o + lane_base, o);
+            tc_fence_before_sync();
+            const bool whole = I.part < 0;
+            float* part = whole ? nullptr : partial_of<N>(a, blockIdx.x, I.part == 0);
+            const int dim = threadIdx.x;
+            int t = 0, h = -1;
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                if (x >= rows) break;
+                if (++h == p.hp) {
+                    h = 0;
+                    ++t;
+                }
+                if (h >= I.nheads) continue;
+                const float L = (red[x] + red[N + x]) + (red[2 * N + x] + red[3 * N + x]);
+                if (whole) {
+                    static_cast<__nv_bfloat16*>(a.out)[(static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + dim] =
+                        __float2bfloat16(o[x] / L);
+                    if (dim == 0) write_lse(a, I, t, h, ref[x], L);
+                } else {
+                    part[x * 128 + dim] = o[x];
+                    if (dim == 0) {
+                        part[N * 128 + x] = ref[x];
+                        part[N * 129 + x] = L;
+                    }
+                }
+            }
+            if (whole) {
+                group_bar();  // red is read
+                continue;
+            }
+            __threadfence();
+            group_bar();
+            if (threadIdx.x == 0) *verdict = last_part(a, I);
+            group_bar();
+            if (!*verdict) continue;
+            // This CTA finished last: it joins the parts.
+            __threadfence();
+            for (int x = 0; x < rows; ++x) {
+                const int t = x / p.hp, h = x - t * p.hp;
+                if (h >= I.nheads) continue;
+                float M = -INFINITY, L = 0.f, acc = 0.f;
+                for (int k0 = 0; k0 < I.n_parts; k0 += 8) {
+                    float pm[8], pl[8], po[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        pm[k] = -INFINITY;
+                        if (k0 + k >= I.n_parts) continue;
+                        const float* src = partial_of<N>(a, I.cta0 + k0 + k, k0 + k == 0);
+                        pm[k] = __ldcg(src + N * 128 + x);
+                        pl[k] = __ldcg(src + N * 129 + x);
+                        po[k] = __ldcg(src + x * 128 + dim);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (pm[k] == -INFINITY) continue;  // no key seen
+                        const float Mn = fmaxf(M, pm[k]);
+                        const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn), f1 = ex2_approx(pm[k] - Mn);
+                        M = Mn;
+                        L = L * f0 + pl[k] * f1;
+                        acc = acc * f0 + po[k] * f1;
+                    }
+                }
+                static_cast<__nv_bfloat16*>(a.out)[(static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + dim] =
+                    __float2bfloat16(acc / L);
+                if (dim == 0) write_lse(a, I, t, h, M, L);
+            }
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 54);
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, C::kTmem);
+}
+
+template <int N>
+cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
+    using C = FewCfg<N>;
+    auto kern = attention_few_kernel<N>;
+    static bool configured = false;  // benign race: the attribute call is idempotent
+    if (!configured) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
+        if (e != cudaSuccess) return e;
+        configured = true;
+    }
+    p.hp = attn_heads_per_tile(L.Hq, L.Hkv, N);
+    p.tp = N / p.hp;
+    p.nhb = (p.G + p.hp - 1) / p.hp;
+    int grid = device_sm_count();
+    if (grid <= 0) return cudaErrorNoDevice;
+    if (L.max_ctas > 0 && L.max_ctas < grid) grid = L.max_ctas;
+    grid *= C::kCtas;
+    if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
+    NvtxRange range("attention_few_kernel");
+    kern<<<grid, kThreadsF, C::kBytes, stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int n,
+                                 cudaStream_t stream) {
+    AttnParams p;
+    p.tmap_k = map_k;
+    p.tmap_v = map_v;
+    p.a = L;
+    p.G = L.Hq / L.Hkv;
+    p.unit_cost = 2;
+    p.min_run = 3;
+    p.page_shift = 0;
+    while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
+    p.c = L.scale * 1.4426950408889634f;
+    p.wait_cycles = wait_limit_cycles();
+    return n == 16 ? launch_few<16>(L, p, stream) : n == 32 ? launch_few<32>(L, p, stream) : launch_few<64>(L, p, stream);
+}
+
+}  // namespace ckv

@@ -1622,7 +1622,7 @@ AttnWs attn_ws_layout() {
     l.counters = sizeof(WsHeader);
     l.ticket = l.counters + kAttnMaxCtas * sizeof(int);
     l.partials = round_up(l.ticket + sizeof(int), kWsAlign);
-    l.total = l.partials + static_cast<size_t>(kAttnMaxCtas) * 2 * attn_partial_floats() * sizeof(float);
+    l.total = l.partials + kAttnPartialFloats * sizeof(float);
     return l;
 }
 
@@ -1703,12 +1703,14 @@ ckv_status make_rows_map(CUtensorMap* map, const void* ptr, int rank, const int6
 }
 
 ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
-    const int hp = attn_heads_per_tile(L.Hq, L.Hkv), tp = kTileKeys / hp;
-    // Two row tiles a unit where the sequences have more rows than one tile on average.
-    const int tiles = static_cast<int64_t>(L.T) > static_cast<int64_t>(L.S) * tp ? 2 : 1;
+    // Over a cache, the kernel for few rows where the sequences have at most 64 (token, head) rows of a KV head
+    // on average; its tiles hold the least power of two that takes them.
+    const int64_t rows = (static_cast<int64_t>(L.T) + L.S - 1) / L.S * (L.Hq / L.Hkv);
+    const int few = !L.paged || rows > 64 ? 0 : rows > 32 ? 64 : rows > 16 ? 32 : 16;
     CUtensorMap mq, mk, mv;
     ckv_status st;
-    {
+    if (!few) {
+        const int hp = attn_heads_per_tile(L.Hq, L.Hkv, kTileKeys), tp = kTileKeys / hp;
         const int64_t dims[3] = {kHeadDim, L.Hq, L.T}, strides[3] = {1, L.q_head, L.q_tok};
         const int box[3] = {64, hp, tp};
         if ((st = make_rows_map(&mq, L.q, 3, dims, strides, box))) return st;
@@ -1728,7 +1730,7 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
         }
         if (st) return st;
     }
-    const cudaError_t e = launch_attention(L, mq, mk, mv, tiles, stream);
+    const cudaError_t e = few ? launch_attention_few(L, mk, mv, few, stream) : launch_attention_tiles(L, mq, mk, mv, stream);
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 

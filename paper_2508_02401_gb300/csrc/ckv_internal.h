@@ -207,9 +207,10 @@ struct SrsLaunch {
 cudaError_t launch_srs_mask(const SrsLaunch& L, cudaStream_t stream);
 cudaError_t launch_srs_span(const SrsLaunch& L, cudaStream_t stream);
 
-// Causal attention (attention.cu): packed prompts, or new tokens over a paged cache.
-constexpr int kAttnMaxCtas = 160;   // CTAs of one launch, and the partial results the workspace holds
-constexpr int kAttnUnitRows = 256;  // query rows (of all heads of a unit) of one CTA, at most
+// Causal attention of packed prompts, or of new tokens over a paged cache.
+constexpr int kAttnMaxCtas = 320, kAttnTilesCtas = 160;  // CTAs of one launch (with 256 rows each)
+// The workspace's partial results: two a CTA, of 256 rows (160 CTAs) or of up to 64 (320), 128 + 2 floats a row.
+constexpr size_t kAttnPartialFloats = static_cast<size_t>(kAttnTilesCtas) * 2 * 256 * 130;
 struct AttnLaunch {
     const void* q;
     int64_t q_tok, q_head;          // strides in elements
@@ -231,16 +232,18 @@ struct AttnLaunch {
     int64_t lse_win_stride;
     int* status;
     int* counters;                  // [kAttnMaxCtas], zero between calls
-    float* partials;                // [kAttnMaxCtas * 2][attn_partial_floats()]
+    float* partials;                // [kAttnPartialFloats]
     bool check_hash;                // cu has to hash to cu_hash
     uint32_t cu_hash;
 };
-// A partial result: an unnormalised output row, its reference maximum and its sum, per unit row.
-constexpr size_t attn_partial_floats() { return static_cast<size_t>(kAttnUnitRows) * (128 + 2); }
-// Query heads of a KV group that share a tile of 128 (token, head) rows.
-constexpr int attn_heads_per_tile(int Hq, int Hkv) { return Hq / Hkv < 128 ? Hq / Hkv : 128; }
-cudaError_t launch_attention(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
-                             const CUtensorMap& map_v, int tiles, cudaStream_t stream);
+// Query heads of a KV group that share a tile of `rows` (token, head) rows.
+constexpr int attn_heads_per_tile(int Hq, int Hkv, int rows) { return Hq / Hkv < rows ? Hq / Hkv : rows; }
+// Two tiles of 128 rows a CTA (attention_tiles.cu).
+cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
+                                   const CUtensorMap& map_v, cudaStream_t stream);
+// n = 16, 32 or 64 rows a CTA, over a paged cache (attention_few.cu).
+cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int n,
+                                 cudaStream_t stream);
 
 // The paged cache (paged_cache.cu).
 struct TablesLaunch {

@@ -69,7 +69,7 @@ class Paged:
         assert ckv.ckv_read_device_status(ws, stream=stream)[0] == status[0]
         out.check()
         lse.check()
-        assert not bool(ws[256:1024].any())
+        assert not bool(ws[256:1536].any())
         return out.view, lse.view
 
     def check(self, **kw):
