@@ -464,33 +464,51 @@ def new_outputs(cfg, layer, batch, device="cuda"):
 
 
 # ------------------------------------------------------------------ attention and the paged cache
-def _need(name, t, dtype, numel=None):
-    """The calls below read and write whole tensors by their sizes, so a tensor of another type, device
-    or size would be read out of bounds: ValueError instead."""
-    import torch
-    if t.dtype != dtype:
-        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
-    if numel is not None and t.numel() < numel:
-        raise ValueError(f"{name} holds {t.numel()} values, {numel} are needed")
+# The calls below read and write whole tensors by their sizes, so a tensor of another type, device or size
+# would be read out of bounds: they raise ValueError instead.  (The smallest of them take 5 us on the GPU,
+# so the checks are kept to a few attribute reads a tensor.)
+_t = None  # torch, once a call needs it
 
 
-def _need_packed(name, t, dtype, numel):
-    _need(name, t, dtype, numel)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
+def _torch():
+    global _t
+    if _t is None:
+        import torch
+        torch.cuda.init()
+        _t = torch
+    return _t
 
 
-def _need_rows(name, t, heads, tok_stride, head_stride):
-    """A [T, heads, 128] bfloat16 tensor; its strides are the ones given, or packed."""
-    import torch
-    _need(name, t, torch.bfloat16)
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
-        raise ValueError(f"{name} is {tuple(t.shape)}, not [T, {heads}, 128]")
-    want = (tok_stride or heads * 128, head_stride or 128, 1)
-    if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
+def _here(stream):
+    """(the current device, the stream handle) of a call."""
+    torch = _t or _torch()
+    dev = torch._C._cuda_getDevice()
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    return dev, stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _packed(name, t, dtype, dev, numel):
+    """The address of a contiguous tensor of at least numel values."""
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < numel or not t.is_contiguous():
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on {t.device}, not on the current CUDA device {dev}")
+        raise ValueError(f"{name} is {tuple(t.shape)} of strides {t.stride()}: {numel} contiguous values are needed")
+    return t.data_ptr()
+
+
+def _rows(name, t, dev, tokens, heads, tok_stride, head_stride):
+    """The address of a [tokens or more, heads, 128] bfloat16 tensor whose strides are the ones given, or packed."""
+    if t.dtype is not _t.bfloat16 or t.get_device() != dev:
+        raise ValueError(f"{name} is {t.dtype} on {t.device}, not bfloat16 on the current CUDA device {dev}")
+    shape, want = t.shape, (tok_stride or heads * 128, head_stride or 128, 1)
+    if len(shape) != 3 or shape[1] != heads or shape[2] != 128 or shape[0] < tokens:
+        raise ValueError(f"{name} is {tuple(shape)}, not [{tokens}, {heads}, 128]")
+    if t.stride() != want and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), want)):
         raise ValueError(f"{name} has strides {t.stride()}, the call says {want}")
+    return t.data_ptr()
 
 
 class PagedCache:
@@ -498,36 +516,42 @@ class PagedCache:
     strided (one buffer [num_pages, 2, page_size, H_kv, 128] for both); a page is packed."""
 
     def __init__(self, k_pages, v_pages):
-        import torch
+        torch = _torch()
         for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-            _need(name, t, torch.bfloat16)
+            if t.dtype is not torch.bfloat16 or not t.is_cuda:
+                raise ValueError(f"{name} is {t.dtype} on {t.device}, not bfloat16 on a CUDA device")
             if t.dim() != 4 or t.shape[3] != 128 or t.shape != k_pages.shape or t.stride() != k_pages.stride():
                 raise ValueError("k_pages and v_pages are [num_pages, page_size, H_kv, 128] of the same strides")
             if t.numel() and t.stride()[1:] != (t.shape[2] * 128, 128, 1):
                 raise ValueError(f"{name}: a page is not packed")
+        if k_pages.device != v_pages.device:
+            raise ValueError("k_pages and v_pages are on different devices")
         self.k_pages, self.v_pages = k_pages, v_pages
+        self.num_pages, self.page_size, self.num_kv_heads = k_pages.shape[:3]
+        self.device_index = k_pages.get_device()
         # (of a single page torch may give any stride)
         stride = k_pages.stride(0) if k_pages.shape[0] > 1 else 0
-        self._c = _PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), stride, k_pages.shape[0], k_pages.shape[1])
-
-    @property
-    def page_size(self) -> int:
-        return self.k_pages.shape[1]
-
-    @property
-    def num_pages(self) -> int:
-        return self.k_pages.shape[0]
-
-    @property
-    def ref(self):
-        return C.byref(self._c)
+        self._c = _PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), stride, self.num_pages, self.page_size)
+        self.ref = C.byref(self._c)
 
 
 def new_paged_cache(cfg, num_pages, page_size, device="cuda"):
     """A PagedCache of uninitialised pages."""
-    import torch
     shape = (num_pages, page_size, cfg.num_kv_heads, 128)
+    torch = _torch()
     return PagedCache(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
+def _cache_of(cfg, cache, dev):
+    if cache.num_kv_heads != cfg.num_kv_heads:
+        raise ValueError(f"the cache has {cache.num_kv_heads} KV heads, the config {cfg.num_kv_heads}")
+    if cache.device_index != dev:
+        raise ValueError(f"the cache is on CUDA device {cache.device_index}, not on the current one, {dev}")
+    return cache.ref
+
+
+def _lse_of(name, lse, dev, heads, rows, stride):
+    return None if lse is None else _packed(name, lse, _t.float32, dev, (heads - 1) * (stride or rows) + rows)
 
 
 def ckv_attention_workspace_size(cfg) -> int:
@@ -538,7 +562,7 @@ def ckv_attention_workspace_size(cfg) -> int:
 
 def new_attention_workspace(cfg, device="cuda"):
     """A zeroed workspace for the attention and paged-cache calls (uint8 tensor)."""
-    import torch
+    torch = _torch()
     return torch.zeros(ckv_attention_workspace_size(cfg), dtype=torch.uint8, device=device)
 
 
@@ -547,87 +571,66 @@ def ckv_prefill_attention(cfg, batch, q, k, v, out, workspace, lse=None, lse_win
                           tok_stride=0, head_stride=0):
     """Causal attention of packed prompts; lse [H_q, T] and lse_win [H_q, S*w] (what the _lse calls
     take) are written where given."""
-    import torch
-    T, Hq, f32 = batch.total_tokens, cfg.num_q_heads, torch.float32
-    _need_rows("q", q, Hq, q_tok_stride, q_head_stride)
-    for name, t in (("k", k), ("v", v)):
-        _need_rows(name, t, cfg.num_kv_heads, tok_stride, head_stride)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t.shape[0] < T:
-            raise ValueError(f"{name} holds {t.shape[0]} tokens, the batch {T}")
-    _need_packed("out", out, torch.bfloat16, T * Hq * 128)
-    if lse is not None:
-        _need_packed("lse", lse, f32, (Hq - 1) * (lse_head_stride or T) + T)
-    if lse_win is not None:
-        rows = batch.num_seqs * cfg.window
-        _need_packed("lse_win", lse_win, f32, (Hq - 1) * (lse_win_head_stride or rows) + rows)
-    _check(load().ckv_prefill_attention(cfg.ref, batch.ref, _ptr(q), q_tok_stride, q_head_stride, _ptr(k),
-                                        _ptr(v), tok_stride, head_stride, _ptr(out), _ptr(lse),
-                                        lse_head_stride, _ptr(lse_win), lse_win_head_stride,
-                                        _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                        _stream(stream)), "ckv_prefill_attention")
+    dev, stream = _here(stream)
+    T, hq, hkv = batch.total_tokens, cfg.num_q_heads, cfg.num_kv_heads
+    rc = (_lib or load()).ckv_prefill_attention(
+        cfg.ref, batch.ref, _rows("q", q, dev, T, hq, q_tok_stride, q_head_stride), q_tok_stride, q_head_stride,
+        _rows("k", k, dev, T, hkv, tok_stride, head_stride), _rows("v", v, dev, T, hkv, tok_stride, head_stride),
+        tok_stride, head_stride, _packed("out", out, _t.bfloat16, dev, T * hq * 128),
+        _lse_of("lse", lse, dev, hq, T, lse_head_stride), lse_head_stride,
+        _lse_of("lse_win", lse_win, dev, hq, batch.num_seqs * cfg.window, lse_win_head_stride), lse_win_head_stride,
+        _packed("workspace", workspace, _t.uint8, dev, 1), workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_prefill_attention")
+
+
+def _table(name, t, rows, dev):
+    if t.dim() != 2 or t.shape[0] != rows:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not [{rows}, max_blocks]")
+    return _packed(name, t, _t.int32, dev, rows)
 
 
 def ckv_block_tables(page_size, cache_lens, new_lens, free_pages, pool, block_table, slot_map, cu_new,
                      lens_out, pool_out, workspace, stream=None):
     """Appends new_lens tokens to every row (-1: gives its pages back): block_table [rows, max_blocks],
     slot_map, cu_new [rows + 1], lens_out and pool_out are written (int32; pool int64 [2])."""
-    import torch
-    n, i32 = cache_lens.numel(), torch.int32
-    for name, t, size in (("cache_lens", cache_lens, n), ("new_lens", new_lens, n), ("free_pages", free_pages, 1),
-                          ("block_table", block_table, n), ("slot_map", slot_map, 0), ("cu_new", cu_new, n + 1),
-                          ("lens_out", lens_out, n)):
-        _need_packed(name, t, i32, size)
-    for name, t in (("pool", pool), ("pool_out", pool_out)):
-        _need_packed(name, t, torch.int64, 2)
-    if block_table.dim() != 2 or block_table.shape[0] != n:
-        raise ValueError(f"block_table is {tuple(block_table.shape)}, not [{n}, max_blocks]")
-    _check(load().ckv_block_tables(page_size, n, _ptr(cache_lens), _ptr(new_lens), _ptr(free_pages),
-                                   free_pages.numel(), _ptr(pool), _ptr(block_table), block_table.shape[1],
-                                   _ptr(slot_map), slot_map.numel(), _ptr(cu_new), _ptr(lens_out),
-                                   _ptr(pool_out), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream(stream)),
-           "ckv_block_tables")
-
-
-def _need_cache(cfg, cache):
-    if cache.k_pages.shape[2] != cfg.num_kv_heads:
-        raise ValueError(f"the cache has {cache.k_pages.shape[2]} KV heads, the config {cfg.num_kv_heads}")
+    dev, stream = _here(stream)
+    n, i32, i64 = cache_lens.numel(), _t.int32, _t.int64
+    rc = (_lib or load()).ckv_block_tables(
+        page_size, n, _packed("cache_lens", cache_lens, i32, dev, n), _packed("new_lens", new_lens, i32, dev, n),
+        _packed("free_pages", free_pages, i32, dev, 1), free_pages.numel(), _packed("pool", pool, i64, dev, 2),
+        _table("block_table", block_table, n, dev), block_table.shape[1],
+        _packed("slot_map", slot_map, i32, dev, 0), slot_map.numel(), _packed("cu_new", cu_new, i32, dev, n + 1),
+        _packed("lens_out", lens_out, i32, dev, n), _packed("pool_out", pool_out, i64, dev, 2),
+        _packed("workspace", workspace, _t.uint8, dev, 1), workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_block_tables")
 
 
 def ckv_cache_write(cfg, cache, k, v, slot_map, workspace, stream=None, tok_stride=0, head_stride=0):
     """k, v [tokens, H_kv, 128] into the cache's slots slot_map [tokens] int32 (-1: skipped)."""
-    import torch
-    _need_cache(cfg, cache)
-    n = slot_map.numel()
-    _need_packed("slot_map", slot_map, torch.int32, n)
-    for name, t in (("k", k), ("v", v)):
-        _need_rows(name, t, cfg.num_kv_heads, tok_stride, head_stride)
-        if t.shape[0] < n:
-            raise ValueError(f"{name} holds {t.shape[0]} tokens, slot_map {n}")
-    _check(load().ckv_cache_write(cfg.ref, cache.ref, n, _ptr(k), _ptr(v), tok_stride, head_stride,
-                                  _ptr(slot_map), _ptr(workspace),
-                                  workspace.numel() * workspace.element_size(), _stream(stream)),
-           "ckv_cache_write")
+    dev, stream = _here(stream)
+    n, hkv = slot_map.numel(), cfg.num_kv_heads
+    rc = (_lib or load()).ckv_cache_write(
+        cfg.ref, _cache_of(cfg, cache, dev), n, _rows("k", k, dev, n, hkv, tok_stride, head_stride),
+        _rows("v", v, dev, n, hkv, tok_stride, head_stride), tok_stride, head_stride,
+        _packed("slot_map", slot_map, _t.int32, dev, n), _packed("workspace", workspace, _t.uint8, dev, 1),
+        workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_cache_write")
 
 
 def ckv_paged_attention(cfg, cache, block_table, cache_lens, cu_new, q, out, workspace, lse=None,
                         lse_head_stride=0, stream=None, q_tok_stride=0, q_head_stride=0):
     """Attention of the new tokens q [tokens, H_q, 128] over the cache: block_table [S, max_blocks],
     cache_lens [S] (new tokens included), cu_new [S + 1] int32, all read on the device."""
-    import torch
-    _need_cache(cfg, cache)
-    S, Hq, T, i32 = cache_lens.numel(), cfg.num_q_heads, q.shape[0], torch.int32
-    _need_rows("q", q, Hq, q_tok_stride, q_head_stride)
-    for name, t, size in (("block_table", block_table, S), ("cache_lens", cache_lens, S), ("cu_new", cu_new, S + 1)):
-        _need_packed(name, t, i32, size)
-    if block_table.dim() != 2 or block_table.shape[0] != S:
-        raise ValueError(f"block_table is {tuple(block_table.shape)}, not [{S}, max_blocks]")
-    _need_packed("out", out, torch.bfloat16, T * Hq * 128)
-    if lse is not None:
-        _need_packed("lse", lse, torch.float32, (Hq - 1) * (lse_head_stride or T) + T)
-    _check(load().ckv_paged_attention(cfg.ref, cache.ref, S, T, _ptr(block_table), block_table.shape[1],
-                                      _ptr(cache_lens), _ptr(cu_new), _ptr(q), q_tok_stride, q_head_stride,
-                                      _ptr(out), _ptr(lse), lse_head_stride, _ptr(workspace),
-                                      workspace.numel() * workspace.element_size(), _stream(stream)),
-           "ckv_paged_attention")
+    dev, stream = _here(stream)
+    S, hq, T, i32 = cache_lens.numel(), cfg.num_q_heads, q.shape[0], _t.int32
+    rc = (_lib or load()).ckv_paged_attention(
+        cfg.ref, _cache_of(cfg, cache, dev), S, T, _table("block_table", block_table, S, dev), block_table.shape[1],
+        _packed("cache_lens", cache_lens, i32, dev, S), _packed("cu_new", cu_new, i32, dev, S + 1),
+        _rows("q", q, dev, T, hq, q_tok_stride, q_head_stride), q_tok_stride, q_head_stride,
+        _packed("out", out, _t.bfloat16, dev, T * hq * 128), _lse_of("lse", lse, dev, hq, T, lse_head_stride),
+        lse_head_stride, _packed("workspace", workspace, _t.uint8, dev, 1), workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_paged_attention")

@@ -332,12 +332,14 @@ __device__ __forceinline__ float* partial_of(const AttnLaunch& a, int cta, bool 
     return a.partials + (static_cast<size_t>(cta) * 2 + (begins ? 1 : 0)) * (ROWS * (kHeadDim + 2));
 }
 
-// Whether this CTA is the last of the unit's parts to arrive (one thread, after its block's writes and fences).
+// Whether this CTA is the last of the unit's parts to arrive: one thread, after a barrier with those that wrote the
+// part and before one with those that join them (a release covers what came before it by barriers, too).
 __device__ __forceinline__ bool last_part(const AttnLaunch& a, const Item& I) {
     int* cnt = a.counters + I.cta0;
-    const bool last = atomicAdd(cnt, 1) == I.n_parts - 1;
+    int n;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(n) : "l"(cnt) : "memory");
+    const bool last = n == I.n_parts - 1;
     if (last) *cnt = 0;  // left zero for the next call
-    __threadfence();
     return last;
 }
 

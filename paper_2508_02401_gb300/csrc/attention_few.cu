@@ -100,11 +100,8 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
         if (threadIdx.x == 0) record_error(a.status, kDevBadIndex, -2);
         return;
     }
-    if (threadIdx.x == 0) *abort = 0;
-    Run run;
-    if (!find_run<kThreadsF>(p, p.tp, heads, scan, run)) return;
-
     if (threadIdx.x == 0) {
+        *abort = 0;
         for (int i = 0; i < C::kRing; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&freed[i], 1);
@@ -134,9 +131,15 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
     // Query rows that a unit does not have are never loaded: zeros (or another unit's rows) in their place.
     for (int i = threadIdx.x; i < 2 * C::kQBytes / 16; i += kThreadsF) reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
+    Run run;
+    const bool busy = find_run<kThreadsF>(p, p.tp, heads, scan, run);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    if (!busy) {
+        if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, C::kTmem);
+        return;
+    }
     const uint32_t tm_s = *tmem_slot, tm_o = tm_s + 2 * N;  // S of even and odd tiles, O
     const long long lim = p.wait_cycles;
 
@@ -438,41 +441,55 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 group_bar();  // red is read
                 continue;
             }
-            __threadfence();
             group_bar();
             if (threadIdx.x == 0) *verdict = last_part(a, I);
             group_bar();
             if (!*verdict) continue;
-            // This CTA finished last: it joins the parts.
-            __threadfence();
-            for (int x = 0; x < rows; ++x) {
-                const int t = x / p.hp, h = x - t * p.hp;
-                if (h >= I.nheads) continue;
-                float M = -INFINITY, L = 0.f, acc = 0.f;
-                for (int k0 = 0; k0 < I.n_parts; k0 += 8) {
-                    float pm[8], pl[8], po[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        pm[k] = -INFINITY;
-                        if (k0 + k >= I.n_parts) continue;
-                        const float* src = partial_of<N>(a, I.cta0 + k0 + k, k0 + k == 0);
-                        pm[k] = __ldcg(src + N * 128 + x);
-                        pl[k] = __ldcg(src + N * 129 + x);
-                        po[k] = __ldcg(src + x * 128 + dim);
+            // This CTA finished last: it joins the parts, a warp a row; a lane holds a part's weight and, of
+            // the row, four dims.
+            for (int x = warp; x < rows; x += 4) {
+                const int tx = x / p.hp, hx = x - tx * p.hp;
+                if (hx >= I.nheads) continue;
+                float M = -INFINITY, L = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k0 = 0; k0 < I.n_parts; k0 += 32) {
+                    const int n = min(32, I.n_parts - k0);
+                    float pm = -INFINITY, pl = 0.f;
+                    if (lane < n) {
+                        const float* src = partial_of<N>(a, I.cta0 + k0 + lane, k0 + lane == 0);
+                        pm = __ldcg(src + N * 128 + x);
+                        pl = __ldcg(src + N * 129 + x);
                     }
+                    const float Mn = fmaxf(M, redux_max(pm));
+                    const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
+                    const float w = pm == -INFINITY ? 0.f : ex2_approx(pm - Mn);  // (0: no key seen)
+                    M = Mn;
+                    L = L * f0 + warp_sum(pl * w);
+                    acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
+#pragma unroll 1
+                    for (int k = 0; k < n; k += 8) {
+                        float4 o[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (pm[k] == -INFINITY) continue;  // no key seen
-                        const float Mn = fmaxf(M, pm[k]);
-                        const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn), f1 = ex2_approx(pm[k] - Mn);
-                        M = Mn;
-                        L = L * f0 + pl[k] * f1;
-                        acc = acc * f0 + po[k] * f1;
+                        for (int y = 0; y < 8; ++y)
+                            o[y] = k + y < n ? __ldcg(reinterpret_cast<const float4*>(
+                                                   partial_of<N>(a, I.cta0 + k0 + k + y, k0 + k + y == 0) + x * 128) + lane)
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            const float wy = __shfl_sync(0xffffffffu, w, (k + y) & 31);
+                            if (k + y >= n) continue;
+                            acc.x += o[y].x * wy;
+                            acc.y += o[y].y * wy;
+                            acc.z += o[y].z * wy;
+                            acc.w += o[y].w * wy;
+                        }
                     }
                 }
-                static_cast<__nv_bfloat16*>(a.out)[(static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + dim] =
-                    __float2bfloat16(acc / L);
-                if (dim == 0) write_lse(a, I, t, h, M, L);
+                const float inv = 1.f / L;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
+                                     (static_cast<long long>(I.q_row + tx) * a.Hq + I.head0 + hx) * kHeadDim + lane * 4;
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                if (lane == 0) write_lse(a, I, tx, hx, M, L);
             }
         }
         if (!ok) {

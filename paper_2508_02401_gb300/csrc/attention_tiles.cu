@@ -117,11 +117,8 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         if (threadIdx.x == 0) record_error(a.status, kDevBadIndex, -2);
         return;
     }
-    if (threadIdx.x == 0) *abort = 0;
-    Run run;
-    if (!find_run<kThreadsT>(p, tq, heads, scan, run)) return;
-
     if (threadIdx.x == 0) {
+        *abort = 0;
         for (int i = 0; i < kRingT; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&freed[i], 1);
@@ -151,9 +148,15 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
+    Run run;
+    const bool busy = find_run<kThreadsT>(p, tq, heads, scan, run);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    if (!busy) {
+        if (warp == kMmaWarp) tmem_dealloc(*tmem_slot, 512);
+        return;
+    }
     // TMEM columns (all are allocated, so they start at 0), + 128 X: the logits S of warpgroup X and, over their
     // first 64, its numerators P in bf16; its output O.
     constexpr uint32_t kTmS = 0, kTmO = 256;
@@ -472,13 +475,11 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 part[kRowsT * 128 + row] = mc;
                 part[kRowsT * 129 + row] = l;
             }
-            __threadfence();
             if (!(ok = pair_sync(pair, pair_phase, abort, lim))) break;
             if (threadIdx.x == 0) *verdict = last_part(a, I);
             if (!(ok = pair_sync(pair, pair_phase, abort, lim))) break;
             if (!*verdict || !valid) continue;
             // This CTA finished last: it joins the parts, a thread its row, part after part.
-            __threadfence();
             float M = 0.f, L = 0.f;
 #pragma unroll 1
             for (int q4 = 0; q4 < 128; q4 += 64) {

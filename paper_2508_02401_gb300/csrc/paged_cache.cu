@@ -32,30 +32,30 @@ __device__ __forceinline__ bool row_counts(const TablesParams& p, int r, int& le
     return len >= 0 && nw >= -1 && len + add <= static_cast<long long>(p.a.max_blocks) << p.shift;
 }
 
-// Exclusive prefix sum over the block's threads; *total is the sum.
-__device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long* total) {
+// Exclusive prefix sums over the block's threads of three values; `total` are the sums.
+__device__ __forceinline__ RowCounts block_scan(const RowCounts& v, RowCounts* warp_sums, RowCounts* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long x = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();  // the previous scan's sums are read
-    if (lane == 31) warp_sums[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        long long s = warp_sums[lane];
+    auto warp_scan = [&](RowCounts x) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
+            const long long a = __shfl_up_sync(0xffffffffu, x.add, o), t = __shfl_up_sync(0xffffffffu, x.take, o),
+                            g = __shfl_up_sync(0xffffffffu, x.give, o);
+            if (lane >= o) {
+                x.add += a;
+                x.take += t;
+                x.give += g;
+            }
         }
-        warp_sums[lane] = s;
-    }
+        return x;
+    };
+    const RowCounts x = warp_scan(v);
+    if (lane == 31) warp_sums[warp] = x;
+    __syncthreads();
+    if (warp == 0) warp_sums[lane] = warp_scan(warp_sums[lane]);
     __syncthreads();
     *total = warp_sums[31];
-    return x - v + (warp ? warp_sums[warp - 1] : 0);
+    const RowCounts b = warp ? warp_sums[warp - 1] : RowCounts{0, 0, 0};
+    return {x.add - v.add + b.add, x.take - v.take + b.take, x.give - v.give + b.give};
 }
 
 // The thread whose share [first[i], first[i + 1]) holds x (shares may be empty; x < first[1024]).
@@ -77,7 +77,7 @@ __device__ __forceinline__ int find_share(const long long* first, long long x) {
 // updated in place; the new blocks' entries and the ring's free part are disjoint from what is read.
 __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_constant__ TablesParams p) {
     __shared__ long long first_tok[kTabThreads + 1], first_page[kTabThreads + 1], first_back[kTabThreads + 1];
-    __shared__ long long warp_sums[32];
+    __shared__ RowCounts warp_sums[32];
     __shared__ int last_s;
     const int n = p.a.n_rows, tid = threadIdx.x;
     const int per = (n + kTabThreads - 1) / kTabThreads;
@@ -95,16 +95,18 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
         sum.take += c.take;
         sum.give += c.give;
     }
-    long long toks, pages, back;
-    first_tok[tid] = block_scan(sum.add, warp_sums, &toks);
-    first_page[tid] = block_scan(sum.take, warp_sums, &pages);
-    first_back[tid] = block_scan(sum.give, warp_sums, &back);
+    const long long taken = p.a.pool[0], returned = p.a.pool[1], cap_pages = p.a.num_pages;
+    RowCounts total;
+    const RowCounts before = block_scan(sum, warp_sums, &total);
+    const long long toks = total.add, pages = total.take, back = total.give;
+    first_tok[tid] = before.add;
+    first_page[tid] = before.take;
+    first_back[tid] = before.give;
     if (tid == 0) {
         first_tok[kTabThreads] = toks;
         first_page[kTabThreads] = pages;
         first_back[kTabThreads] = back;
     }
-    const long long taken = p.a.pool[0], returned = p.a.pool[1], cap_pages = p.a.num_pages;
     const bool bad_rows = __syncthreads_or(bad);
     int why = 0;  // the status detail
     if (bad_rows) why = 1;
@@ -116,6 +118,8 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
     const bool ok = why == 0;
     if (!ok && blockIdx.x == 0 && tid == 0) record_error(p.a.status, kDevPool, why);
 
+    // ring positions of the first page taken and given back; from there on less than one round
+    const long long take0 = ok ? taken % cap_pages : 0, give0 = ok ? returned % cap_pages : 0;
     const int P1 = (1 << p.shift) - 1;
     const long long a = blockIdx.x * p.seg;
     const long long b = min(a + p.seg, static_cast<long long>(p.a.cap));
@@ -139,7 +143,8 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
             if (block < have) {
                 page = *entry;
             } else {
-                page = p.a.free_pages[(taken + page0 + (block - have)) % cap_pages];
+                const long long x = take0 + page0 + (block - have);
+                page = p.a.free_pages[x < cap_pages ? x : x - cap_pages];
                 if ((pos & P1) == 0) *entry = page;
             }
             if (page < 0 || page >= p.a.num_pages) record_error(p.a.status, kDevBadIndex, r);
@@ -159,7 +164,8 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
                 if (x < at + c.give) break;
                 at += c.give;
             }
-            p.a.free_pages[(returned + x) % cap_pages] =
+            const long long to = give0 + x;
+            p.a.free_pages[to < cap_pages ? to : to - cap_pages] =
                 p.a.table[static_cast<size_t>(r) * p.a.max_blocks + (x - at)];
         }
     }
