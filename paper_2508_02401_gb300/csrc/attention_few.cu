@@ -56,16 +56,39 @@ __device__ __forceinline__ bool group_or(bool x) {
     return r != 0;
 }
 
-template <int N>
-__device__ __forceinline__ void tmem_ldn(uint32_t taddr, float (&v)[N]) {
+// COLS (4, 8 or a multiple of 16) columns of a thread's lane; complete on return.
+template <int COLS>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float* v) {
+    if constexpr (COLS == 4) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(taddr) : "memory");
+    } else if constexpr (COLS == 8) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                     : "r"(taddr) : "memory");
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; i += 16) tmem_ld16_nowait(taddr + i, reinterpret_cast<float(&)[16]>(v[i]));
+        for (int i = 0; i < COLS; i += 16) tmem_ld16_nowait(taddr + i, reinterpret_cast<float(&)[16]>(v[i]));
+    }
     tmem_ld_wait();
 #pragma unroll
-    for (int i = 0; i < N; i += 16) reg_fence(reinterpret_cast<float(&)[16]>(v[i]));
+    for (int i = 0; i < COLS; ++i) asm volatile("" : "+f"(v[i]));
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const float* v) {
+    if constexpr (COLS == 4) {
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                     "f"(v[3]) : "memory");
+    } else if constexpr (COLS == 8) {
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "f"(v[0]), "f"(v[1]),
+                     "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+    } else {
+        tmem_st16(taddr, reinterpret_cast<const float(&)[16]>(*v));
+    }
 }
 
-template <int N>
+// COLS of the N columns hold rows (4, 8 or 16 of 16): the others' numerators stay zero.
+template <int N, int COLS>
 __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_kernel(const __grid_constant__ AttnParams p) {
     using C = FewCfg<N>;
     constexpr uint32_t kIdescS = idesc_bf16_f32(128, N);
@@ -129,7 +152,9 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
         tmem_relinquish();
     }
     // Query rows that a unit does not have are never loaded: zeros (or another unit's rows) in their place.
-    for (int i = threadIdx.x; i < 2 * C::kQBytes / 16; i += kThreadsF) reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
+    static_assert(C::kP == C::kQ + 2 * C::kQBytes, "P follows the query buffers");
+    for (int i = threadIdx.x; i < (2 * C::kQBytes + C::kPBytes) / 16; i += kThreadsF)
+        reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     Run run;
     const bool busy = find_run<kThreadsF>(p, p.tp, heads, scan, run);
@@ -201,8 +226,10 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
         }
     } else if (warp == kMmaWarpF) {
         // ---------------------------------------------------------------- MMA issuer
-        // The logits of a tile (of the next item's first) before the product of the one before it: S has two buffers,
-        // and the numerators of a tile are there only when its S has been read.
+        // The logits of a tile before the product of the one before it: S has two buffers, and the numerators of a
+        // tile are there only when its S has been read.  An item's first logits come after the last product of the
+        // one before it, whose result would otherwise wait for a K still on its way (256 caches of 300 tokens: 72 -> 67
+        // us).
         constexpr uint32_t kTileUnits = kTileBytes >> 4;
         const uint32_t ring_addr = desc_addr(ring), q_addr = desc_addr(qbuf), p_lo = desc_addr(pbuf) | (1u << 16);
         uint32_t sn = 0, pn = 0, cs = 0, cph = 0;  // logits and products issued; ring slot and phase of the next K
@@ -252,9 +279,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 const bool last = i == n - 1;
                 if (last && !(ok = fetch())) break;
                 // ring: K(i) V(i) K(i + 1)
-                if (!last) ok = qk(2, false, i + 2 == n);
-                else if (!end_) ok = qk(2, true, n_ == 1);
-                if (!ok) break;
+                if (!last && !(ok = qk(2, false, i + 2 == n))) break;
                 const uint32_t vs = slot_of(1);
                 const uint32_t v_lo = uniform((ring_addr + vs * kTileUnits) | kDescLoV), d_tmem = uniform(tm_o);
                 const uint32_t accumulate = uniform(i > 0);
@@ -273,6 +298,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                     umma_commit(&freed[vs]);
                 }
                 __syncwarp();
+                if (last && !end_) ok = qk(2, true, n_ == 1);
                 cph = phase_of(2);
                 cs = slot_of(2);
             }
@@ -295,7 +321,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
         const float c = p.c;
         uint32_t sn = 0;
         bool ok = true;
-        float l[N];  // this thread's keys' sums
+        float l[COLS];  // this thread's keys' sums
         // The product of the tile before the current one is in O, and its numerators have been read.
         auto wait_pv = [&](uint32_t tile) {
             if (tile == 0) return;
@@ -312,8 +338,8 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
             if (lane == 0) mbar_arrive(&item_free[slot]);
             if (I.part == kEndItem) break;
 #pragma unroll
-            for (int x = 0; x < N; ++x) l[x] = 0.f;
-            if (key < N) ref[key] = -INFINITY;
+            for (int x = 0; x < COLS; ++x) l[x] = 0.f;
+            if (key < COLS) ref[key] = -INFINITY;
             group_bar();
             const int rows = I.ntok * p.hp;
             // The first key that some row does not see.
@@ -323,13 +349,13 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 tile_wait(&s_full[sn & 1], (sn >> 1) & 1, abort, lim, a.status);
                 __syncwarp();
                 tc_fence_after_sync();
-                float s[N];
-                tmem_ldn<N>(tm_s + (sn & 1) * N + lane_base, s);
+                float s[COLS];
+                tmem_load<COLS>(tm_s + (sn & 1) * N + lane_base, s);
                 tc_fence_before_sync();
                 if (k0 + kTileKeys > first_end) {
                     int ends = first_end - (k0 + key), h = 0;  // positive: the row of column x sees the key
 #pragma unroll
-                    for (int x = 0; x < N; ++x) {
+                    for (int x = 0; x < COLS; ++x) {
                         s[x] = ends > 0 ? s[x] : -INFINITY;
                         if (++h == p.hp) {
                             h = 0;
@@ -339,61 +365,62 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 }
                 float over = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < N; ++x) {
+                for (int x = 0; x < COLS; ++x) {
                     s[x] *= c;
                     over = fmaxf(over, x < rows ? s[x] - ref[x] : -INFINITY);
                 }
-                const bool moved = group_or(over > kAttnTau);
-                wait_pv(sn);
-                if (moved) {
+                if (group_or(over > kAttnTau)) {
+                    wait_pv(sn);
                     // Move the references that a key passes by more than 2^8 (or that have none yet).
 #pragma unroll
-                    for (int x = 0; x < N; ++x) {
+                    for (int x = 0; x < COLS; ++x) {
                         const float w = redux_max(s[x]);
-                        if (lane == 0) red[warp * N + x] = w;
+                        if (lane == 0) red[warp * COLS + x] = w;
                     }
                     group_bar();
+                    constexpr int kStep = COLS < 16 ? COLS : 16;
 #pragma unroll
-                    for (int x0 = 0; x0 < N; x0 += 16) {
-                        float o[16];
-                        if (i > 0) {
-                            tmem_ld16_nowait(tm_o + lane_base + x0, o);
-                            tmem_ld_wait();
-                            reg_fence(o);
-                        }
+                    for (int x0 = 0; x0 < COLS; x0 += kStep) {
+                        float o[kStep];
+                        if (i > 0) tmem_load<kStep>(tm_o + lane_base + x0, o);
 #pragma unroll
-                        for (int x = x0; x < x0 + 16; ++x) {
-                            const float mx = fmaxf(fmaxf(red[x], red[N + x]), fmaxf(red[2 * N + x], red[3 * N + x]));
+                        for (int x = x0; x < x0 + kStep; ++x) {
+                            const float mx = fmaxf(fmaxf(red[x], red[COLS + x]), fmaxf(red[2 * COLS + x], red[3 * COLS + x]));
                             // (false for -inf - -inf)
                             const float f = mx - ref[x] > kAttnTau ? ex2_approx(ref[x] - mx) : 1.f;
                             l[x] *= f;
                             o[x - x0] *= f;
                         }
-                        if (i > 0) tmem_st16(tm_o + lane_base + x0, o);
+                        if (i > 0) tmem_store<kStep>(tm_o + lane_base + x0, o);
                     }
                     tmem_st_wait();
                     tc_fence_before_sync();
                     group_bar();  // ref is read
-                    if (key < N) {
-                        const float mx = fmaxf(fmaxf(red[key], red[N + key]), fmaxf(red[2 * N + key], red[3 * N + key]));
+                    if (key < COLS) {
+                        const float mx = fmaxf(fmaxf(red[key], red[COLS + key]), fmaxf(red[2 * COLS + key], red[3 * COLS + key]));
                         if (mx - ref[key] > kAttnTau) ref[key] = mx;
                     }
                     group_bar();
                 }
-                uint32_t pk[N / 2];
+                uint32_t pk[COLS / 2];
 #pragma unroll
-                for (int x = 0; x < N; ++x) {
+                for (int x = 0; x < COLS; ++x) {
                     s[x] = ex2_approx(s[x] - fmaxf(ref[x], -3e38f));  // (-inf: a row that has seen no key yet)
                     l[x] += s[x];
                 }
 #pragma unroll
-                for (int x = 0; x < N; x += 2) pk[x >> 1] = pack_bf16(s[x], s[x + 1]);
+                for (int x = 0; x < COLS; x += 2) pk[x >> 1] = pack_bf16(s[x], s[x + 1]);
+                wait_pv(sn);  // the last tile's numerators are read
                 // The key's row of P, its 16-byte pieces swizzled by the address bits above the row's.
+                uint8_t* prow = pbuf + key * (2 * N);
+                const int sw = N == 16 ? (key >> 2) & 1 : (N == 32 ? (key >> 1) & 3 : key & 7);
+                if constexpr (COLS == 4) {
+                    *reinterpret_cast<uint2*>(prow + (sw << 4)) = make_uint2(pk[0], pk[1]);
+                } else {
 #pragma unroll
-                for (int x = 0; x < N / 8; ++x) {
-                    const int sw = N == 16 ? (key >> 2) & 1 : (N == 32 ? (key >> 1) & 3 : key & 7);
-                    *reinterpret_cast<uint4*>(pbuf + key * (2 * N) + ((x ^ sw) << 4)) =
-                        make_uint4(pk[4 * x], pk[4 * x + 1], pk[4 * x + 2], pk[4 * x + 3]);
+                    for (int x = 0; x < COLS / 8; ++x)
+                        *reinterpret_cast<uint4*>(prow + ((x ^ sw) << 4)) =
+                            make_uint4(pk[4 * x], pk[4 * x + 1], pk[4 * x + 2], pk[4 * x + 3]);
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -401,33 +428,48 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 __syncwarp();
             }
             // ---- the unit's (or this part's) result: the rows' sums over the threads, then a dim a thread
+            if constexpr (COLS >= 8) {
+                float none[COLS];
 #pragma unroll
-            for (int x = 0; x < N; ++x) {
-                if (x >= rows) break;
-                const float w = warp_sum(l[x]);
-                if (lane == 0) red[warp * N + x] = w;
+                for (int x = 0; x < COLS; ++x) none[x] = 0.f;
+                if constexpr (COLS <= 32) {
+                    transpose_reduce<COLS>(l, none, lane);  // lane: column lane / (32 / COLS)
+                    if (lane % (32 / COLS) == 0) red[warp * COLS + lane / (32 / COLS)] = l[0];
+                } else {
+                    transpose_reduce<32>(reinterpret_cast<float(&)[32]>(l[0]), reinterpret_cast<float(&)[32]>(none[0]), lane);
+                    transpose_reduce<32>(reinterpret_cast<float(&)[32]>(l[32]), reinterpret_cast<float(&)[32]>(none[32]), lane);
+                    red[warp * COLS + lane] = l[0];
+                    red[warp * COLS + 32 + lane] = l[32];
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) l[x] = warp_sum(l[x]);
+                if (lane == 0) {
+#pragma unroll
+                    for (int x = 0; x < COLS; ++x) red[warp * COLS + x] = l[x];
+                }
             }
             wait_pv(sn);
             group_bar();
-            float o[N];
-            tmem_ldn<N>(tm_o + lane_base, o);
+            float o[COLS];
+            tmem_load<COLS>(tm_o + lane_base, o);
             tc_fence_before_sync();
             const bool whole = I.part < 0;
             float* part = whole ? nullptr : partial_of<N>(a, blockIdx.x, I.part == 0);
             const int dim = threadIdx.x;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<long long>(I.q_row) * a.Hq + I.head0) * kHeadDim + dim;
             int t = 0, h = -1;
 #pragma unroll
-            for (int x = 0; x < N; ++x) {
+            for (int x = 0; x < COLS; ++x) {
                 if (x >= rows) break;
                 if (++h == p.hp) {
                     h = 0;
                     ++t;
                 }
                 if (h >= I.nheads) continue;
-                const float L = (red[x] + red[N + x]) + (red[2 * N + x] + red[3 * N + x]);
+                const float L = (red[x] + red[COLS + x]) + (red[2 * COLS + x] + red[3 * COLS + x]);
                 if (whole) {
-                    static_cast<__nv_bfloat16*>(a.out)[(static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + dim] =
-                        __float2bfloat16(o[x] / L);
+                    out[(t * a.Hq + h) * kHeadDim] = __float2bfloat16(o[x] * (1.f / L));
                     if (dim == 0) write_lse(a, I, t, h, ref[x], L);
                 } else {
                     part[x * 128 + dim] = o[x];
@@ -503,18 +545,18 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
     if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, C::kTmem);
 }
 
-template <int N>
+template <int N, int COLS>
 cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
     using C = FewCfg<N>;
-    auto kern = attention_few_kernel<N>;
+    auto kern = attention_few_kernel<N, COLS>;
     static bool configured = false;  // benign race: the attribute call is idempotent
     if (!configured) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
         if (e != cudaSuccess) return e;
         configured = true;
     }
-    p.hp = attn_heads_per_tile(L.Hq, L.Hkv, N);
-    p.tp = N / p.hp;
+    p.hp = attn_heads_per_tile(L.Hq, L.Hkv, COLS);
+    p.tp = COLS / p.hp;
     p.nhb = (p.G + p.hp - 1) / p.hp;
     int grid = device_sm_count();
     if (grid <= 0) return cudaErrorNoDevice;
@@ -528,7 +570,7 @@ cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) 
 
 }  // namespace
 
-cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int n,
+cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int rows,
                                  cudaStream_t stream) {
     AttnParams p;
     p.tmap_k = map_k;
@@ -536,12 +578,15 @@ cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, 
     p.a = L;
     p.G = L.Hq / L.Hkv;
     p.unit_cost = 2;
-    p.min_run = 3;
+    p.min_run = 1;
     p.page_shift = 0;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
     p.wait_cycles = wait_limit_cycles();
-    return n == 16 ? launch_few<16>(L, p, stream) : n == 32 ? launch_few<32>(L, p, stream) : launch_few<64>(L, p, stream);
+    if (rows <= 4) return launch_few<16, 4>(L, p, stream);
+    if (rows <= 8) return launch_few<16, 8>(L, p, stream);
+    if (rows <= 16) return launch_few<16, 16>(L, p, stream);
+    return rows <= 32 ? launch_few<32, 32>(L, p, stream) : launch_few<64, 64>(L, p, stream);
 }
 
 }  // namespace ckv

@@ -1704,9 +1704,9 @@ ckv_status make_rows_map(CUtensorMap* map, const void* ptr, int rank, const int6
 
 ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // Over a cache, the kernel for few rows where the sequences have at most 64 (token, head) rows of a KV head
-    // on average; its tiles hold the least power of two that takes them.
+    // on average.
     const int64_t rows = (static_cast<int64_t>(L.T) + L.S - 1) / L.S * (L.Hq / L.Hkv);
-    const int few = !L.paged || rows > 64 ? 0 : rows > 32 ? 64 : rows > 16 ? 32 : 16;
+    const bool few = L.paged && rows <= 64;
     CUtensorMap mq, mk, mv;
     ckv_status st;
     if (!few) {
@@ -1730,7 +1730,7 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
         }
         if (st) return st;
     }
-    const cudaError_t e = few ? launch_attention_few(L, mk, mv, few, stream) : launch_attention_tiles(L, mq, mk, mv, stream);
+    const cudaError_t e = few ? launch_attention_few(L, mk, mv, static_cast<int>(rows), stream) : launch_attention_tiles(L, mq, mk, mv, stream);
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 

@@ -241,8 +241,9 @@ constexpr int attn_heads_per_tile(int Hq, int Hkv, int rows) { return Hq / Hkv <
 // Two tiles of 128 rows a CTA (attention_tiles.cu).
 cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
                                    const CUtensorMap& map_v, cudaStream_t stream);
-// n = 16, 32 or 64 rows a CTA, over a paged cache (attention_few.cu).
-cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int n,
+// Over a paged cache, units of 4, 8, 16, 32 or 64 rows: the least that takes `rows` (at most 64), the rows that a
+// sequence has on average (attention_few.cu).
+cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int rows,
                                  cudaStream_t stream);
 
 // The paged cache (paged_cache.cu).
