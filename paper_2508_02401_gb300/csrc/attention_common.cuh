@@ -180,13 +180,24 @@ __device__ __forceinline__ long long cost_before(const AttnParams& p, const Seq&
     return j == nj && nj > 0 ? s + unit_tiles(q, tq, nj - 1) : s;
 }
 
-// This CTA's run: positions [w0, w1) of the line, of W over `ctas` CTAs.
+// This CTA's run: positions [w0, w1) of the line, of W over `ctas` CTAs; CTA b's begins at floor(b W / ctas).
 struct Run {
-    long long w0, w1, W, ctas;
+    long long w0, w1, W;
+    int ctas;
+    // the CTA of position x
+    __device__ int cta_of(long long x) const { return static_cast<int>(((x + 1) * ctas - 1) / W); }
 };
+// Where it begins: sequence s, and w0's offset in it.
+struct RunStart {
+    long long offset;
+    Seq q;
+    int s;
+};
+constexpr int kScanBytes = 14 * 8 + static_cast<int>(sizeof(RunStart));
 
-// Whole block; false (for all of it): nothing to do.  `scan` (16 long long in shared memory) is left with the
-// sequence that holds w0 and w0's offset in it at [14], [15], to be read after the next barrier.
+// Whole block; false (for all of it): nothing to do.  `scan`: kScanBytes of shared memory, the RunStart in it
+// to be read after the next barrier.
+__device__ __forceinline__ RunStart* run_start(long long* scan) { return reinterpret_cast<RunStart*>(scan + 14); }
 template <int THREADS>
 __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads, long long* scan, Run& r) {
     static_assert(THREADS / 32 <= 14, "scan");
@@ -196,14 +207,17 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
     const int per = (a.S + THREADS - 1) / THREADS;
     const int s_lo = min(static_cast<long long>(threadIdx.x) * per, static_cast<long long>(a.S));
     const int s_hi = min(s_lo + per, a.S);
-    auto cost = [&](int s, bool& bad, bool report) {
-        const Seq q = get_seq(a, s, cu0, bad, report);
+    auto cost = [&](const Seq& q) {
         const int nj = (q.n + tq - 1) / tq;
         return q.n > 0 ? heads * cost_before(p, q, tq, nj, nj) : 0ll;
     };
     long long own = 0;
     bool bad = false;
-    for (int s = s_lo; s < s_hi; ++s) own += cost(s, bad, blockIdx.x == 0);
+    Seq q{0, 0, 0};
+    for (int s = s_lo; s < s_hi; ++s) {
+        q = get_seq(a, s, cu0, bad, blockIdx.x == 0);
+        own += cost(q);
+    }
     long long incl = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -224,23 +238,29 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
         else if (bad) record_error(a.status, kDevBadIndex, -1);
     }
     if (bad || r.W == 0) return false;
-    r.ctas = (r.W + p.min_run - 1) / p.min_run;
-    if (r.ctas > gridDim.x) r.ctas = gridDim.x;
-    if (blockIdx.x >= r.ctas) return false;
-    r.w0 = blockIdx.x * r.W / r.ctas;
-    r.w1 = (blockIdx.x + 1) * r.W / r.ctas;
+    const long long most = (r.W + p.min_run - 1) / p.min_run;
+    r.ctas = most < gridDim.x ? static_cast<int>(most) : static_cast<int>(gridDim.x);
+    const int b = blockIdx.x;
+    if (b >= r.ctas) return false;
+    const long long each = r.W / r.ctas;
+    const int left = static_cast<int>(r.W - each * r.ctas);
+    r.w0 = each * b + b * left / r.ctas;
+    r.w1 = each * (b + 1) + (b + 1) * left / r.ctas;
     if (r.w0 >= before && r.w0 < before + own) {  // the thread whose sequences hold w0
-        long long at = before;
-        for (int s = s_lo; s < s_hi; ++s) {
-            bool ignore = false;
-            const long long w = cost(s, ignore, false);
-            if (r.w0 < at + w) {
-                scan[14] = s;
-                scan[15] = r.w0 - at;
-                break;
+        RunStart* st = run_start(scan);
+        int s = s_lo;
+        if (per > 1) {
+            for (;; ++s) {
+                bool ignore = false;
+                q = get_seq(a, s, cu0, ignore, false);
+                const long long w = cost(q);
+                if (r.w0 < before + w) break;
+                before += w;
             }
-            at += w;
         }
+        st->offset = r.w0 - before;
+        st->q = q;
+        st->s = s;
     }
     return true;
 }
@@ -251,18 +271,17 @@ struct Walk {
     const Run& r;
     const int tq, heads;
     Seq q;
-    int s, cu0, nj, j, hb, t0;
-    long long at;  // the position of tile t0
+    int s, nj, j, hb, t0, kt;  // kt: key tiles of row tile j
+    long long at;              // the position of tile t0
 
-    __device__ Walk(const AttnParams& p_, const Run& r_, int tq_, int heads_, const long long* scan)
+    __device__ Walk(const AttnParams& p_, const Run& r_, int tq_, int heads_, long long* scan)
         : p(p_), r(r_), tq(tq_), heads(heads_) {
-        bool ignore = false;
-        cu0 = p.a.cu[0];
-        s = static_cast<int>(scan[14]);
-        q = get_seq(p.a, s, cu0, ignore, false);
+        const RunStart* st = run_start(scan);
+        s = st->s;
+        q = st->q;
         nj = (q.n + tq - 1) / tq;
-        long long off = scan[15];
-        int lo = 0, hi = nj;  // the row tile that holds `off`: 32 candidates at a time
+        long long off = st->offset;
+        int lo = 0, hi = nj;  // the row tile that holds the offset: 32 candidates at a time
         while (hi - lo > 1) {
             const int step = (hi - lo + 31) / 32, cand = lo + (threadIdx.x & 31) * step;
             const bool le = cand < hi && heads * cost_before(p, q, tq, cand, nj) <= off;
@@ -270,8 +289,9 @@ struct Walk {
             hi = min(hi, lo + step);
         }
         j = lo;
-        off -= heads * cost_before(p, q, tq, j, nj);
-        const int cost = unit_tiles(q, tq, j) + p.unit_cost;
+        if (j > 0) off -= heads * cost_before(p, q, tq, j, nj);
+        kt = unit_tiles(q, tq, j);
+        const int cost = kt + p.unit_cost;
         hb = static_cast<int>(off / cost);
         t0 = static_cast<int>(off - static_cast<long long>(hb) * cost);
         at = r.w0 + max(0, p.unit_cost - t0);
@@ -280,13 +300,29 @@ struct Walk {
 
     // Item::n is left to the kernel.
     __device__ bool next(Item& I) {
+        if (t0 == kt) {  // the next unit
+            t0 = 0;
+            if (++hb == heads) {
+                hb = 0;
+                if (++j == nj && at < r.w1) {
+                    j = 0;
+                    bool ignore = false;
+                    const int cu0 = p.a.cu[0];
+                    do {
+                        if (++s >= p.a.S) break;
+                        q = get_seq(p.a, s, cu0, ignore, false);
+                    } while (q.n <= 0);
+                    nj = (q.n + tq - 1) / tq;
+                }
+                if (at < r.w1) kt = unit_tiles(q, tq, j);
+            }
+        }
         if (at >= r.w1) {
             I.part = kEndItem;
             return false;
         }
-        const int kt = unit_tiles(q, tq, j);
         const int t1 = static_cast<int>(min(static_cast<long long>(kt), t0 + (r.w1 - at)));
-        const int g = hb / p.nhb, b = hb - g * p.nhb;
+        const int g = p.nhb == 1 ? hb : hb / p.nhb, b = hb - g * p.nhb;
         I.ntok = min(tq, q.n - j * tq);
         I.q_row = q.row0 + j * tq;
         I.pos0 = q.len - q.n + j * tq;
@@ -301,26 +337,14 @@ struct Walk {
         I.part = -1;
         I.n_parts = 1;
         I.cta0 = 0;
-        if (t0 > 0 || t1 < kt) {  // the CTA of position x is floor(((x + 1) ctas - 1) / W)
+        if (t0 > 0 || t1 < kt) {
             const long long u0 = at - t0;
-            I.cta0 = static_cast<int>(((u0 + 1) * r.ctas - 1) / r.W);
-            I.n_parts = static_cast<int>(((u0 + kt) * r.ctas - 1) / r.W) - I.cta0 + 1;
+            I.cta0 = r.cta_of(u0);
+            I.n_parts = r.cta_of(u0 + kt - 1) - I.cta0 + 1;
             I.part = static_cast<int>(blockIdx.x) - I.cta0;
         }
         at += I.n_tiles + p.unit_cost;
-        t0 = 0;
-        if (++hb == heads) {
-            hb = 0;
-            if (++j == nj) {
-                j = 0;
-                bool ignore = false;
-                do {
-                    if (++s >= p.a.S) break;
-                    q = get_seq(p.a, s, cu0, ignore, false);
-                } while (q.n <= 0);
-                nj = (q.n + tq - 1) / tq;
-            }
-        }
+        t0 = kt;
         return true;
     }
 };

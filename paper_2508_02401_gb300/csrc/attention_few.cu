@@ -36,7 +36,7 @@ struct FewCfg {
                          kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 1, kItemFull = kPvDone + 1,
                          kItemFree = kItemFull + kAttnItemRing, kDone = kItemFree + kAttnItemRing, kNumBars = kDone + 1;
     static constexpr int kScan = kBars + 8 * ((kNumBars + 1) & ~1);
-    static constexpr int kMisc = kScan + 8 * 16;
+    static constexpr int kMisc = kScan + kScanBytes;
     static constexpr int kBytes = kMisc + 16;
     static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * N * 130 <= kAttnPartialFloats, "workspace");
     static_assert(kBytes <= (kCtas == 2 ? 115712 : 232448), "shared memory");

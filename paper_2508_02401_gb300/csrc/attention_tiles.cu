@@ -30,8 +30,8 @@ struct TilesSmem {
                          kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 2, kTurn = kPvDone + 2,
                          kItemFull = kTurn + 2, kItemFree = kItemFull + kAttnItemRing,
                          kPair = kItemFree + kAttnItemRing, kDone = kPair + 1, kNumBars = kDone + 1;
-    static constexpr int kScan = kBars + 8 * kNumBars;  // long long [16]
-    static constexpr int kMisc = kScan + 8 * 16;        // TMEM base, abort, verdict
+    static constexpr int kScan = kBars + 8 * kNumBars;
+    static constexpr int kMisc = kScan + kScanBytes;  // TMEM base, abort, verdict
     static constexpr int kBytes = kMisc + 16;
 };
 static_assert(TilesSmem::kBytes <= 232448, "shared memory");
