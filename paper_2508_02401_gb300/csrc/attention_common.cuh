@@ -233,10 +233,7 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
         if (i < warp) before += scan[i];
         r.W += scan[i];
     }
-    if (blockIdx.x == 0 && threadIdx.x == THREADS - 1) {
-        if (a.check_hash && seqlens_hash(a.cu, a.S) != a.cu_hash) record_error(a.status, kDevBadSeqlens, 120);
-        else if (bad) record_error(a.status, kDevBadIndex, -1);
-    }
+    if (bad && blockIdx.x == 0 && threadIdx.x == 0) record_error(a.status, kDevBadIndex, -1);
     if (bad || r.W == 0) return false;
     const long long most = (r.W + p.min_run - 1) / p.min_run;
     r.ctas = most < gridDim.x ? static_cast<int>(most) : static_cast<int>(gridDim.x);
@@ -263,6 +260,18 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
         st->s = s;
     }
     return true;
+}
+
+// Whether cu on the device is the host's copy (seqlens_hash, by a whole warp: some 30 cycles an entry, which is why
+// a warp without another job does it).
+__device__ __forceinline__ void check_seqlens(const AttnLaunch& a) {
+    const int lane = threadIdx.x & 31;
+    uint32_t h = 2166136261u;
+    for (int i0 = 0; i0 <= a.S; i0 += 32) {
+        const uint32_t v = i0 + lane <= a.S ? static_cast<uint32_t>(a.cu[i0 + lane]) : 0u;
+        for (int i = 0; i < 32 && i0 + i <= a.S; ++i) h = (h ^ __shfl_sync(0xffffffffu, v, i)) * 16777619u;
+    }
+    if (lane == 0 && h != a.cu_hash) record_error(a.status, kDevBadSeqlens, 120);
 }
 
 // The items of a run, one after the other (a whole warp).
@@ -453,6 +462,19 @@ struct TileLoader {
         for (uint32_t k = use > RING ? use - RING : 0; k < use; ++k) mbar_wait(&full[k % RING], (k / RING) & 1, &never);
     }
 };
+
+// Host: lets a kernel have its shared memory, once a device (a benign race: the call is idempotent).
+constexpr int kAttnMaxDevices = 64;
+template <class Kernel>
+cudaError_t attn_configure(Kernel kern, int bytes, bool (&configured)[kAttnMaxDevices]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < kAttnMaxDevices && configured[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < kAttnMaxDevices) configured[dev] = true;
+    return e;
+}
 
 }  // namespace
 }  // namespace ckv

@@ -549,12 +549,9 @@ template <int N, int COLS>
 cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
     using C = FewCfg<N>;
     auto kern = attention_few_kernel<N, COLS>;
-    static bool configured = false;  // benign race: the attribute call is idempotent
-    if (!configured) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
-        if (e != cudaSuccess) return e;
-        configured = true;
-    }
+    static bool configured[kAttnMaxDevices] = {};
+    const cudaError_t e = attn_configure(kern, C::kBytes, configured);
+    if (e != cudaSuccess) return e;
     p.hp = attn_heads_per_tile(L.Hq, L.Hkv, COLS);
     p.tp = COLS / p.hp;
     p.nhb = (p.G + p.hp - 1) / p.hp;

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreadsT = 384;
 constexpr int kRingT = 5;  // K and V tiles of 32 KB
-constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 0-3, 4-7: softmax; 8, 9: the MMAs of either; 11: idle
+constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 0-3, 4-7: softmax; 8, 9: the MMAs of either
 constexpr int kRowsT = 256;
 static_assert(static_cast<size_t>(kAttnTilesCtas) * 2 * kRowsT * 130 <= kAttnPartialFloats, "workspace");
 
@@ -332,6 +332,8 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         } else if (warp < kLoadWarp) {
             if (warp == kMmaWarp) mma_role(std::integral_constant<int, 0>{});
             else mma_role(std::integral_constant<int, 1>{});
+        } else if (a.check_hash && blockIdx.x == 0) {
+            check_seqlens(a);
         }
     } else {
         // ---------------------------------------------------------------- softmax, a row a thread
@@ -533,12 +535,9 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
 template <bool PAGED>
 cudaError_t launch_variant(const AttnParams& p, int grid, cudaStream_t stream) {
     auto kern = attention_tiles_kernel<PAGED>;
-    static bool configured = false;  // benign race: the attribute call is idempotent
-    if (!configured) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TilesSmem::kBytes);
-        if (e != cudaSuccess) return e;
-        configured = true;
-    }
+    static bool configured[kAttnMaxDevices] = {};
+    const cudaError_t e = attn_configure(kern, TilesSmem::kBytes, configured);
+    if (e != cudaSuccess) return e;
     NvtxRange range("attention_tiles_kernel");
     kern<<<grid, kThreadsT, TilesSmem::kBytes, stream>>>(p);
     return cudaGetLastError();
