@@ -38,6 +38,7 @@ struct alignas(128) AttnParams {
     int G, hp, tp, nhb;  // heads of a KV group; heads and tokens of a row tile; head blocks of a group
     int unit_cost;       // what a unit costs beside its key tiles, in key tiles
     int min_run;         // length of a CTA's run, at least
+    float join_cost;     // what the join of a unit's part costs, in key tiles (0: nothing to speak of)
     int page_shift;
     float c;             // scale * log2(e)
     long long wait_cycles;
@@ -193,7 +194,7 @@ struct RunStart {
     Seq q;
     int s;
 };
-constexpr int kScanBytes = 14 * 8 + static_cast<int>(sizeof(RunStart));
+constexpr int kScanBytes = 14 * 8 + static_cast<int>(sizeof(RunStart)) + 14 * 4;
 
 // Whole block; false (for all of it): nothing to do.  `scan`: kScanBytes of shared memory, the RunStart in it
 // to be read after the next barrier.
@@ -211,31 +212,44 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
         const int nj = (q.n + tq - 1) / tq;
         return q.n > 0 ? heads * cost_before(p, q, tq, nj, nj) : 0ll;
     };
+    int* scan_units = reinterpret_cast<int*>(run_start(scan) + 1);
     long long own = 0;
+    int units = 0;
     bool bad = false;
     Seq q{0, 0, 0};
     for (int s = s_lo; s < s_hi; ++s) {
         q = get_seq(a, s, cu0, bad, blockIdx.x == 0);
         own += cost(q);
+        units += (q.n + tq - 1) / tq;
     }
+    units = __reduce_add_sync(0xffffffffu, units);
     long long incl = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long y = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += y;
     }
-    if (lane == 31) scan[warp] = incl;
+    if (lane == 31) {
+        scan[warp] = incl;
+        scan_units[warp] = units;
+    }
     bad = __syncthreads_or(bad);
     long long before = incl - own;
     r.W = 0;
+    units = 0;
 #pragma unroll
     for (int i = 0; i < THREADS / 32; ++i) {
         if (i < warp) before += scan[i];
         r.W += scan[i];
+        units += scan_units[i];
     }
     if (bad && blockIdx.x == 0 && threadIdx.x == 0) record_error(a.status, kDevBadIndex, -1);
     if (bad || r.W == 0) return false;
-    const long long most = (r.W + p.min_run - 1) / p.min_run;
+    // A unit of k tiles in runs of r of them takes r and its k / r parts' joins: least at r = sqrt(k join_cost).
+    int least = p.min_run;
+    if (p.join_cost > 0.f)
+        least = max(least, static_cast<int>(sqrtf(p.join_cost * static_cast<float>(r.W) / (static_cast<float>(units) * heads))));
+    const long long most = (r.W + least - 1) / least;
     r.ctas = most < gridDim.x ? static_cast<int>(most) : static_cast<int>(gridDim.x);
     const int b = blockIdx.x;
     if (b >= r.ctas) return false;
@@ -377,7 +391,8 @@ __device__ __forceinline__ bool last_part(const AttnLaunch& a, const Item& I) {
 }
 
 __device__ __forceinline__ void write_lse(const AttnLaunch& a, const Item& I, int tok, int head, float mc, float l) {
-    const float lse = (mc + log2f(l)) * 0.6931471805599453f;
+    if (!a.lse && !a.lse_win) return;
+    const float lse = (mc + lg2_approx(l)) * 0.6931471805599453f;  // (2^-22 of absolute error in the logarithm)
     const int t = I.q_row + tok, h = I.head0 + head;
     if (a.lse) a.lse[h * a.lse_stride + t] = lse;
     if (a.lse_win) {

@@ -576,6 +576,7 @@ cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, 
     p.G = L.Hq / L.Hkv;
     p.unit_cost = 2;
     p.min_run = 1;
+    p.join_cost = 0.f;
     p.page_shift = 0;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;

@@ -558,6 +558,7 @@ cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q
     p.nhb = (p.G + p.hp - 1) / p.hp;
     p.unit_cost = 3;
     p.min_run = 4;
+    p.join_cost = 1.f;
     p.page_shift = 0;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
