@@ -277,8 +277,8 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
 }
 
 // Whether cu on the device is the host's copy (seqlens_hash, by a whole warp: some 30 cycles an entry, which is why
-// a warp without another job does it).
-__device__ __forceinline__ void check_seqlens(const AttnLaunch& a) {
+// a warp without another job does it; not inlined: beside the tiles kernel's loops it cost them 5%).
+__device__ __noinline__ void check_seqlens(const AttnLaunch& a) {
     const int lane = threadIdx.x & 31;
     uint32_t h = 2166136261u;
     for (int i0 = 0; i0 <= a.S; i0 += 32) {
