@@ -410,8 +410,9 @@ CKV_API ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer,
  * ckv_block_tables -> ckv_cache_write -> ckv_paged_attention.  (The paper's own decoding over the
  * compressed cache is Eq. 3-4; its prefill attention is Eq. 2.)
  *
- * The workspace of these calls is ckv_attention_workspace_size's, zeroed once like the others; the
- * rules above for workspaces, streams, alignment and errors hold.  Of the config they read the head
+ * The workspace of these calls is ckv_attention_workspace_size's, zeroed once like the others, and again
+ * after a status of code 2 (a wait that gave up can leave the count of a unit's parts open); the rules
+ * above for workspaces, streams, alignment and errors hold.  Of the config they read the head
  * counts, window, softmax_scale and max_ctas.  fp32 logits, sums and outputs' accumulation; the
  * softmax's numerators are rounded to bf16 for the product with v, as the outputs are at the end.
  * Logits are below 1e8 in magnitude.  v is finite: a NaN or an infinity in a value row can reach query
