@@ -1,13 +1,13 @@
 // Attention of a few query rows a sequence over a paged cache (attention_common.cuh): single tokens, short drafts.
 //
-// With G heads of one token on a KV head, 128 rows of the MMA would hold G; so the keys take the MMA's M and the
-// N (token, head) rows its N: S^T [128 keys][N] = K Q^T, a key a thread, and O^T [128 dims][N] += V^T P with the
-// numerators P [128 keys][N] in shared memory.  Every thread has N exponentials a tile, the rows' sums stay in the
-// threads until a unit's end, and the reference of a row is moved by the warps together when a vote says so.
+// With G heads of one token on a KV head, 128 rows of the MMA would hold G; so the keys take the MMA's M and up to
+// 16 (token, head) rows its N: S^T [128 keys][16] = K Q^T, a key a thread, and O^T [128 dims][16] += V^T P with the
+// numerators P [128 keys][16] in shared memory.  The rows' sums stay in the threads until a unit's end, and the
+// references are moved by the warps together when a vote says so.
 //
-// Bound by the loads of K and V: 64 KB a key tile, 1.5 us of an SM's share of the bandwidth, against some 0.6 us of
-// the path K tile - logits - numerators - product.  With N = 16 two CTAs run on an SM, so that one's start and end
-// of a unit lie beside the other's loads.
+// Bound by the loads of K and V: 64 KB a key tile, 1.5 us of an SM's share of the bandwidth (8 caches of 131072
+// tokens, 4.3 GB: 620 us, 6.9 TB/s).  Two CTAs run on an SM, so that one's start and end of a unit lie beside the
+// other's loads; what they do not hide shows on short caches (256 of 300 tokens, 319 MB: 62 us).
 #include "attention_common.cuh"
 
 namespace ckv {
@@ -16,31 +16,30 @@ namespace {
 constexpr int kThreadsF = 256;
 constexpr int kMmaWarpF = 4, kLoadWarpF = 5, kQWarpF = 6;  // warps 0-3: softmax; 7: idle
 
-template <int N>
-struct FewCfg {
-    static constexpr int kCtas = N == 16 ? 2 : 1;                  // on an SM
-    static constexpr int kRing = N == 16 ? 3 : (N == 32 ? 6 : 5);  // K and V tiles of 32 KB
-    static constexpr int kQBytes = N * 256;                        // two buffers
-    static constexpr int kPBytes = N * 256;
-    static constexpr int kTmem = N == 16 ? 64 : 4 * N;             // columns: two S, one O
-    // P as the MMA's B: rows of 2 N bytes a key, swizzled over as many bytes; 8-key groups
-    static constexpr uint32_t kPGroup = 16 * N;
-    static constexpr uint32_t kPHi = (kPGroup >> 4) | (1u << 14) | ((N == 16 ? 6u : (N == 32 ? 4u : 2u)) << 29);
-    static constexpr int kQ = kRing * kTileBytes;
-    static constexpr int kP = kQ + 2 * kQBytes;
-    static constexpr int kRed = kP + kPBytes;   // float [4][N]
-    static constexpr int kRef = kRed + 16 * N;  // float [N]: the rows' references, times c
-    static constexpr int kItems = kRef + 4 * N;
+constexpr int kN = 16;        // (token, head) columns of the MMAs
+constexpr int kCtasF = 2;     // on an SM
+constexpr int kRingF = 3;     // K and V tiles of 32 KB
+constexpr int kQBytesF = kN * 256, kPBytesF = kN * 256;
+constexpr int kTmemF = 64;    // columns: two S, one O (48)
+// P as the second MMA's B: rows of 32 bytes a key, swizzled over as many; 8-key groups of 256 bytes.
+constexpr uint32_t kPGroup = 256, kPHi = (kPGroup >> 4) | (1u << 14) | (6u << 29);
+
+struct FewSmem {
+    static constexpr int kQ = kRingF * kTileBytes;
+    static constexpr int kP = kQ + 2 * kQBytesF;
+    static constexpr int kRed = kP + kPBytesF;   // float [4][kN]
+    static constexpr int kRef = kRed + 16 * kN;  // float [kN]: the rows' references, times c
+    static constexpr int kItems = kRef + 4 * kN;
     static constexpr int kBars = kItems + kAttnItemRing * static_cast<int>(sizeof(Item));
-    static constexpr int kFull = 0, kFree = kFull + kRing, kQFull = kFree + kRing, kQFree = kQFull + 2,
+    static constexpr int kFull = 0, kFree = kFull + kRingF, kQFull = kFree + kRingF, kQFree = kQFull + 2,
                          kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 1, kItemFull = kPvDone + 1,
                          kItemFree = kItemFull + kAttnItemRing, kDone = kItemFree + kAttnItemRing, kNumBars = kDone + 1;
-    static constexpr int kScan = kBars + 8 * ((kNumBars + 1) & ~1);
+    static constexpr int kScan = kBars + 8 * kNumBars;
     static constexpr int kMisc = kScan + kScanBytes;
     static constexpr int kBytes = kMisc + 16;
-    static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * N * 130 <= kAttnPartialFloats, "workspace");
-    static_assert(kBytes <= (kCtas == 2 ? 115712 : 232448), "shared memory");
 };
+static_assert(FewSmem::kBytes <= 115712, "shared memory of two CTAs");
+static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * kN * 130 <= kAttnPartialFloats, "workspace");
 
 // Barriers of the softmax warps.  None leaves without the others: they agree on every item, and no wait for a
 // tile makes one leave.
@@ -56,7 +55,7 @@ __device__ __forceinline__ bool group_or(bool x) {
     return r != 0;
 }
 
-// COLS (4, 8 or a multiple of 16) columns of a thread's lane; complete on return.
+// COLS (4, 8 or 16) columns of a thread's lane; complete on return.
 template <int COLS>
 __device__ __forceinline__ void tmem_load(uint32_t taddr, float* v) {
     if constexpr (COLS == 4) {
@@ -67,8 +66,7 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, float* v) {
                      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
                      : "r"(taddr) : "memory");
     } else {
-#pragma unroll
-        for (int i = 0; i < COLS; i += 16) tmem_ld16_nowait(taddr + i, reinterpret_cast<float(&)[16]>(v[i]));
+        tmem_ld16_nowait(taddr, reinterpret_cast<float(&)[16]>(*v));
     }
     tmem_ld_wait();
 #pragma unroll
@@ -87,12 +85,12 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const float* v) {
     }
 }
 
-// COLS of the N columns hold rows (4, 8 or 16 of 16): the others' numerators stay zero.
-template <int N, int COLS>
-__global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_kernel(const __grid_constant__ AttnParams p) {
-    using C = FewCfg<N>;
-    constexpr uint32_t kIdescS = idesc_bf16_f32(128, N);
-    constexpr uint32_t kIdescO = idesc_bf16_f32(128, N) | (1u << 15) | (1u << 16);  // A and B with M, N contiguous
+// COLS of the 16 columns hold rows (4, 8 or 16): the others' numerators stay zero.
+template <int COLS>
+__global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const __grid_constant__ AttnParams p) {
+    using C = FewSmem;
+    constexpr uint32_t kIdescS = idesc_bf16_f32(128, kN);
+    constexpr uint32_t kIdescO = idesc_bf16_f32(128, kN) | (1u << 15) | (1u << 16);  // A and B with M, N contiguous
     extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t* ring = sm;
     uint8_t* qbuf = sm + C::kQ;
@@ -125,7 +123,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
     }
     if (threadIdx.x == 0) {
         *abort = 0;
-        for (int i = 0; i < C::kRing; ++i) {
+        for (int i = 0; i < kRingF; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&freed[i], 1);
         }
@@ -148,12 +146,12 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
         tma_prefetch_desc(&p.tmap_v);
     }
     if (warp == kMmaWarpF) {
-        tmem_alloc(tmem_slot, C::kTmem);
+        tmem_alloc(tmem_slot, kTmemF);
         tmem_relinquish();
     }
     // Query rows that a unit does not have are never loaded: zeros (or another unit's rows) in their place.
-    static_assert(C::kP == C::kQ + 2 * C::kQBytes, "P follows the query buffers");
-    for (int i = threadIdx.x; i < (2 * C::kQBytes + C::kPBytes) / 16; i += kThreadsF)
+    static_assert(C::kP == C::kQ + 2 * kQBytesF, "P follows the query buffers");
+    for (int i = threadIdx.x; i < (2 * kQBytesF + kPBytesF) / 16; i += kThreadsF)
         reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     Run run;
@@ -162,16 +160,16 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
     __syncthreads();
     tc_fence_after_sync();
     if (!busy) {
-        if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, C::kTmem);
+        if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, kTmemF);
         return;
     }
-    const uint32_t tm_s = *tmem_slot, tm_o = tm_s + 2 * N;  // S of even and odd tiles, O
+    const uint32_t tm_s = *tmem_slot, tm_o = tm_s + 2 * kN;  // S of even and odd tiles, O
     const long long lim = p.wait_cycles;
 
     if (warp == kLoadWarpF) {
         // ---------------------------------------------------------------- items, K and V tiles
         Walk walk(p, run, p.tp, heads, scan);
-        TileLoader<true, C::kRing> tiles{p, ring, full, freed, abort, lim};
+        TileLoader<true, kRingF> tiles{p, ring, full, freed, abort, lim};
         bool ok = true;
         for (int it = 0; ok; ++it) {
             const int slot = it % kAttnItemRing;
@@ -204,7 +202,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
             if (I.part == kEndItem) break;
             if (!(ok = warp_wait(&q_free[qs], ((it >> 1) & 1) ^ 1, abort, lim))) break;
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
-            uint8_t* dst = qbuf + qs * C::kQBytes;
+            uint8_t* dst = qbuf + qs * kQBytesF;
             const int chunks = I.ntok * p.hp * 16;
 #pragma unroll 4
             for (int x = lane; x < chunks; x += 32) {
@@ -213,7 +211,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 if (h >= I.nheads) continue;
                 const uint4 val = *reinterpret_cast<const uint4*>(
                     src + (I.q_row + t) * a.q_tok + (I.head0 + h) * a.q_head + ch * 8);
-                *reinterpret_cast<uint4*>(dst + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
+                *reinterpret_cast<uint4*>(dst + (ch >> 3) * (kN * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -247,14 +245,14 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
             ++it;
             return true;
         };
-        auto slot_of = [&](uint32_t d) { return cs + d >= C::kRing ? cs + d - C::kRing : cs + d; };
-        auto phase_of = [&](uint32_t d) { return cs + d >= C::kRing ? cph ^ 1 : cph; };
+        auto slot_of = [&](uint32_t d) { return cs + d >= kRingF ? cs + d - kRingF : cs + d; };
+        auto phase_of = [&](uint32_t d) { return cs + d >= kRingF ? cph ^ 1 : cph; };
         auto qk = [&](uint32_t d, bool first, bool last) {  // K at ring position d; item it - 1
             const uint32_t ks = slot_of(d), qs = (it - 1) & 1;
             if (first && !warp_wait(&q_full[qs], ((it - 1) >> 1) & 1, abort, lim)) return false;
             const uint32_t k_lo = uniform((ring_addr + ks * kTileUnits) | kDescLoK);
-            const uint32_t q_lo = uniform((q_addr + qs * (C::kQBytes >> 4)) | kDescLoK);
-            const uint32_t d_tmem = uniform(tm_s + (sn & 1) * N);
+            const uint32_t q_lo = uniform((q_addr + qs * (kQBytesF >> 4)) | kDescLoK);
+            const uint32_t d_tmem = uniform(tm_s + (sn & 1) * kN);
             tile_wait(&full[ks], phase_of(d), abort, lim, a.status);
             __syncwarp();
             tc_fence_after_sync();
@@ -262,7 +260,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
                     umma_ss<kDescHi>(d_tmem, k_lo + (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2,
-                                     q_lo + (kk >> 2) * (N * 128 >> 4) + (kk & 3) * 2, kIdescS, kk > 0 ? 1u : 0u);
+                                     q_lo + (kk >> 2) * (kN * 128 >> 4) + (kk & 3) * 2, kIdescS, kk > 0 ? 1u : 0u);
                 umma_commit(&s_full[sn & 1]);
                 umma_commit(&freed[ks]);
                 if (last) umma_commit(&q_free[qs]);
@@ -292,7 +290,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
-                        umma_ss<C::kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * C::kPGroup >> 4), kIdescO,
+                        umma_ss<kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * kPGroup >> 4), kIdescO,
                                          kk > 0 ? 1u : accumulate);
                     umma_commit(pv_done);
                     umma_commit(&freed[vs]);
@@ -350,7 +348,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 __syncwarp();
                 tc_fence_after_sync();
                 float s[COLS];
-                tmem_load<COLS>(tm_s + (sn & 1) * N + lane_base, s);
+                tmem_load<COLS>(tm_s + (sn & 1) * kN + lane_base, s);
                 tc_fence_before_sync();
                 if (k0 + kTileKeys > first_end) {
                     int ends = first_end - (k0 + key), h = 0;  // positive: the row of column x sees the key
@@ -378,21 +376,16 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                         if (lane == 0) red[warp * COLS + x] = w;
                     }
                     group_bar();
-                    constexpr int kStep = COLS < 16 ? COLS : 16;
+                    float o[COLS];
+                    if (i > 0) tmem_load<COLS>(tm_o + lane_base, o);
 #pragma unroll
-                    for (int x0 = 0; x0 < COLS; x0 += kStep) {
-                        float o[kStep];
-                        if (i > 0) tmem_load<kStep>(tm_o + lane_base + x0, o);
-#pragma unroll
-                        for (int x = x0; x < x0 + kStep; ++x) {
-                            const float mx = fmaxf(fmaxf(red[x], red[COLS + x]), fmaxf(red[2 * COLS + x], red[3 * COLS + x]));
-                            // (false for -inf - -inf)
-                            const float f = mx - ref[x] > kAttnTau ? ex2_approx(ref[x] - mx) : 1.f;
-                            l[x] *= f;
-                            o[x - x0] *= f;
-                        }
-                        if (i > 0) tmem_store<kStep>(tm_o + lane_base + x0, o);
+                    for (int x = 0; x < COLS; ++x) {
+                        const float mx = fmaxf(fmaxf(red[x], red[COLS + x]), fmaxf(red[2 * COLS + x], red[3 * COLS + x]));
+                        const float f = mx - ref[x] > kAttnTau ? ex2_approx(ref[x] - mx) : 1.f;  // (no: -inf - -inf)
+                        l[x] *= f;
+                        o[x] *= f;
                     }
+                    if (i > 0) tmem_store<COLS>(tm_o + lane_base, o);
                     tmem_st_wait();
                     tc_fence_before_sync();
                     group_bar();  // ref is read
@@ -412,8 +405,8 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 for (int x = 0; x < COLS; x += 2) pk[x >> 1] = pack_bf16(s[x], s[x + 1]);
                 wait_pv(sn);  // the last tile's numerators are read
                 // The key's row of P, its 16-byte pieces swizzled by the address bits above the row's.
-                uint8_t* prow = pbuf + key * (2 * N);
-                const int sw = N == 16 ? (key >> 2) & 1 : (N == 32 ? (key >> 1) & 3 : key & 7);
+                uint8_t* prow = pbuf + key * (2 * kN);
+                const int sw = (key >> 2) & 1;
                 if constexpr (COLS == 4) {
                     *reinterpret_cast<uint2*>(prow + (sw << 4)) = make_uint2(pk[0], pk[1]);
                 } else {
@@ -432,15 +425,8 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 float none[COLS];
 #pragma unroll
                 for (int x = 0; x < COLS; ++x) none[x] = 0.f;
-                if constexpr (COLS <= 32) {
-                    transpose_reduce<COLS>(l, none, lane);  // lane: column lane / (32 / COLS)
-                    if (lane % (32 / COLS) == 0) red[warp * COLS + lane / (32 / COLS)] = l[0];
-                } else {
-                    transpose_reduce<32>(reinterpret_cast<float(&)[32]>(l[0]), reinterpret_cast<float(&)[32]>(none[0]), lane);
-                    transpose_reduce<32>(reinterpret_cast<float(&)[32]>(l[32]), reinterpret_cast<float(&)[32]>(none[32]), lane);
-                    red[warp * COLS + lane] = l[0];
-                    red[warp * COLS + 32 + lane] = l[32];
-                }
+                transpose_reduce<COLS>(l, none, lane);  // lane: column lane / (32 / COLS)
+                if (lane % (32 / COLS) == 0) red[warp * COLS + lane / (32 / COLS)] = l[0];
             } else {
 #pragma unroll
                 for (int x = 0; x < COLS; ++x) l[x] = warp_sum(l[x]);
@@ -455,7 +441,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
             tmem_load<COLS>(tm_o + lane_base, o);
             tc_fence_before_sync();
             const bool whole = I.part < 0;
-            float* part = whole ? nullptr : partial_of<N>(a, blockIdx.x, I.part == 0);
+            float* part = whole ? nullptr : partial_of<kN>(a, blockIdx.x, I.part == 0);
             const int dim = threadIdx.x;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<long long>(I.q_row) * a.Hq + I.head0) * kHeadDim + dim;
             int t = 0, h = -1;
@@ -474,8 +460,8 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                 } else {
                     part[x * 128 + dim] = o[x];
                     if (dim == 0) {
-                        part[N * 128 + x] = ref[x];
-                        part[N * 129 + x] = L;
+                        part[kN * 128 + x] = ref[x];
+                        part[kN * 129 + x] = L;
                     }
                 }
             }
@@ -498,9 +484,9 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
                     const int n = min(32, I.n_parts - k0);
                     float pm = -INFINITY, pl = 0.f;
                     if (lane < n) {
-                        const float* src = partial_of<N>(a, I.cta0 + k0 + lane, k0 + lane == 0);
-                        pm = __ldcg(src + N * 128 + x);
-                        pl = __ldcg(src + N * 129 + x);
+                        const float* src = partial_of<kN>(a, I.cta0 + k0 + lane, k0 + lane == 0);
+                        pm = __ldcg(src + kN * 128 + x);
+                        pl = __ldcg(src + kN * 129 + x);
                     }
                     const float Mn = fmaxf(M, redux_max(pm));
                     const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
@@ -514,7 +500,7 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
 #pragma unroll
                         for (int y = 0; y < 8; ++y)
                             o[y] = k + y < n ? __ldcg(reinterpret_cast<const float4*>(
-                                                   partial_of<N>(a, I.cta0 + k0 + k + y, k0 + k + y == 0) + x * 128) + lane)
+                                                   partial_of<kN>(a, I.cta0 + k0 + k + y, k0 + k + y == 0) + x * 128) + lane)
                                              : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                         for (int y = 0; y < 8; ++y) {
@@ -542,15 +528,14 @@ __global__ void __launch_bounds__(kThreadsF, FewCfg<N>::kCtas) attention_few_ker
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, C::kTmem);
+    if (warp == kMmaWarpF) tmem_dealloc(*tmem_slot, kTmemF);
 }
 
-template <int N, int COLS>
+template <int COLS>
 cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
-    using C = FewCfg<N>;
-    auto kern = attention_few_kernel<N, COLS>;
+    auto kern = attention_few_kernel<COLS>;
     static bool configured[kAttnMaxDevices] = {};
-    const cudaError_t e = attn_configure(kern, C::kBytes, configured);
+    const cudaError_t e = attn_configure(kern, FewSmem::kBytes, configured);
     if (e != cudaSuccess) return e;
     p.hp = attn_heads_per_tile(L.Hq, L.Hkv, COLS);
     p.tp = COLS / p.hp;
@@ -558,10 +543,10 @@ cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) 
     int grid = device_sm_count();
     if (grid <= 0) return cudaErrorNoDevice;
     if (L.max_ctas > 0 && L.max_ctas < grid) grid = L.max_ctas;
-    grid *= C::kCtas;
+    grid *= kCtasF;
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
     NvtxRange range("attention_few_kernel");
-    kern<<<grid, kThreadsF, C::kBytes, stream>>>(p);
+    kern<<<grid, kThreadsF, FewSmem::kBytes, stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -581,10 +566,8 @@ cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, 
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
     p.wait_cycles = wait_limit_cycles();
-    if (rows <= 4) return launch_few<16, 4>(L, p, stream);
-    if (rows <= 8) return launch_few<16, 8>(L, p, stream);
-    if (rows <= 16) return launch_few<16, 16>(L, p, stream);
-    return rows <= 32 ? launch_few<32, 32>(L, p, stream) : launch_few<64, 64>(L, p, stream);
+    // Only the columns in use are worked on: 256 caches of 300 tokens, 4 rows each, 61.9 us with 4 columns, 67.1 with 16.
+    return rows <= 4 ? launch_few<4>(L, p, stream) : rows <= 8 ? launch_few<8>(L, p, stream) : launch_few<16>(L, p, stream);
 }
 
 }  // namespace ckv

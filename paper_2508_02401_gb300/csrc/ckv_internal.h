@@ -209,7 +209,7 @@ cudaError_t launch_srs_span(const SrsLaunch& L, cudaStream_t stream);
 
 // Causal attention of packed prompts, or of new tokens over a paged cache.
 constexpr int kAttnMaxCtas = 320, kAttnTilesCtas = 160;  // CTAs of one launch (with 256 rows each)
-// The workspace's partial results: two a CTA, of 256 rows (160 CTAs) or of up to 64 (320), 128 + 2 floats a row.
+// The workspace's partial results: two a CTA, of 256 rows (160 CTAs) or of 16 (320), 128 + 2 floats a row.
 constexpr size_t kAttnPartialFloats = static_cast<size_t>(kAttnTilesCtas) * 2 * 256 * 130;
 struct AttnLaunch {
     const void* q;
@@ -241,8 +241,8 @@ constexpr int attn_heads_per_tile(int Hq, int Hkv, int rows) { return Hq / Hkv <
 // Two tiles of 128 rows a CTA (attention_tiles.cu).
 cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
                                    const CUtensorMap& map_v, cudaStream_t stream);
-// Over a paged cache, units of 4, 8, 16, 32 or 64 rows: the least that takes `rows` (at most 64), the rows that a
-// sequence has on average (attention_few.cu).
+// Over a paged cache, units of 4, 8 or 16 rows: the least that takes `rows`, the rows that a sequence has on
+// average (attention_few.cu).
 cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int rows,
                                  cudaStream_t stream);
 
