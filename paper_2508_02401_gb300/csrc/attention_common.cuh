@@ -205,9 +205,9 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
     const AttnLaunch& a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cu0 = a.cu[0];
-    const int per = (a.S + THREADS - 1) / THREADS;
+    const int per = (a.S - 1) / THREADS + 1;
     const int s_lo = min(static_cast<long long>(threadIdx.x) * per, static_cast<long long>(a.S));
-    const int s_hi = min(s_lo + per, a.S);
+    const int s_hi = s_lo + min(per, a.S - s_lo);
     auto cost = [&](const Seq& q) {
         const int nj = (q.n + tq - 1) / tq;
         return q.n > 0 ? heads * cost_before(p, q, tq, nj, nj) : 0ll;

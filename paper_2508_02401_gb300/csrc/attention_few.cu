@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                 } else {
                     part[x * 128 + dim] = o[x];
                     if (dim == 0) {
-                        part[kN * 128 + x] = ref[x];
+                        part[kN * 128 + x] = L == 0.f ? ref[x] : fmaxf(ref[x], -3e38f);  // (only NaN seen: joined)
                         part[kN * 129 + x] = L;
                     }
                 }
@@ -540,10 +540,10 @@ cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) 
     p.hp = attn_heads_per_tile(L.Hq, L.Hkv, COLS);
     p.tp = COLS / p.hp;
     p.nhb = (p.G + p.hp - 1) / p.hp;
-    int grid = device_sm_count();
-    if (grid <= 0) return cudaErrorNoDevice;
-    if (L.max_ctas > 0 && L.max_ctas < grid) grid = L.max_ctas;
-    grid *= kCtasF;
+    const int sms = device_sm_count();
+    if (sms <= 0) return cudaErrorNoDevice;
+    int grid = sms * kCtasF;
+    if (L.max_ctas > 0 && L.max_ctas < sms) grid = L.max_ctas;  // (two could go to an SM each)
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
     NvtxRange range("attention_few_kernel");
     kern<<<grid, kThreadsF, FewSmem::kBytes, stream>>>(p);

@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 ++items_done;
             }
             tc_fence_after_sync();
-            if (m == -INFINITY) mc = -INFINITY;  // the row saw no key here
+            if (m == -INFINITY && l == 0.f) mc = -INFINITY;  // the row saw no key here (or, with a NaN in l, only NaN)
             // ---- the unit's (or this part's) result
             const bool whole = I.part < 0;
             float* part = whole ? nullptr : partial_of<kRowsT>(a, blockIdx.x, I.part == 0);

@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
     __shared__ RowCounts warp_sums[32];
     __shared__ int last_s;
     const int n = p.a.n_rows, tid = threadIdx.x;
-    const int per = (n + kTabThreads - 1) / kTabThreads;
-    const int r0 = min(static_cast<long long>(tid) * per, static_cast<long long>(n)), r1 = min(r0 + per, n);
+    const int per = (n - 1) / kTabThreads + 1;
+    const int r0 = min(static_cast<long long>(tid) * per, static_cast<long long>(n)), r1 = r0 + min(per, n - r0);
     bool bad = false;
     RowCounts sum{0, 0, 0};
     for (int r = r0; r < r1; ++r) {

@@ -111,6 +111,25 @@ def test_long_caches_are_cut_and_joined(new, max_ctas):
     Paged(config(8, 2, max_ctas=max_ctas), (20011, 77, 9000), (new, new, 1), 64, seed=6).check()
 
 
+@pytest.mark.parametrize("new", [1, 70])
+def test_nan_keys_in_one_part(new):
+    """A stretch of NaN keys as long as a part of a cut unit makes the rows that see it NaN."""
+    c = Paged(config(8, 2), (9001, 500), (new, 1), 32, seed=17)
+    pages = dev(c.table[0], torch.int64)[64:160]
+    c.k_pages[pages] = math.nan
+    out, lse = c.run()
+    assert bool(out[:new].isnan().all()) and bool(lse[:, :new].isnan().all())
+    assert not bool(out[new:].isnan().any()) and not bool(lse[:, new:].isnan().any())
+
+
+def test_many_sequences():
+    """More sequences than the plan has threads, empty ones among them."""
+    g = np.random.default_rng(3)
+    lens = [int(x) for x in g.integers(0, 40, 1500)]
+    new = [min(n, int(x)) for n, x in zip(lens, g.integers(0, 3, 1500))]
+    Paged(config(4, 1), lens, new, 16, seed=18, pad=3).check()
+
+
 def test_growing_maxima_over_the_cut():
     """Each key tile's logits above the last one's: every part of a cut unit has another reference."""
     c = Paged(config(8, 2), (9001,), (2,), 32, seed=7)

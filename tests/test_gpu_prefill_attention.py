@@ -95,6 +95,13 @@ def test_capped_grid(max_ctas):
           normal(T, 2, 128, seed=3))
 
 
+def test_many_prompts():
+    """More sequences than the plan has threads, empty ones among them."""
+    lens = tuple(int(x) for x in np.random.default_rng(3).integers(0, 9, 900))
+    T = sum(lens)
+    check(config(2, 1, window=8), lens, normal(T, 2, 128, seed=1), normal(T, 1, 128, seed=2), normal(T, 1, 128, seed=3))
+
+
 def test_one_long_prompt_per_cta_split():
     """Few row tiles and many keys: units are cut over CTAs and joined."""
     lens = (6001,)
@@ -180,6 +187,17 @@ def test_masked_keys_of_any_value():
         kk[333:] = bad
         got = run(config(), (T,), q, kk, v)
         assert torch.equal(got[0][:333], want[0][:333]) and torch.equal(got[1][:, :333], want[1][:, :333])
+
+
+@pytest.mark.parametrize("span", [(0, 1), (256, 640), (0, 4096), (4000, 4096)])
+def test_nan_keys_that_rows_see(span):
+    """NaN keys, a tile's or a part's worth of them: every row that sees one is NaN, in out and lse."""
+    T, hq = 4500, 2  # few row tiles: their keys are cut over CTAs
+    cfg, q, k, v = config(hq, 1), normal(T, hq, 128, seed=1), normal(T, 1, 128, seed=2), normal(T, 1, 128, seed=3)
+    k[span[0]:span[1]] = math.nan
+    out, lse, _ = run(cfg, (T,), q, k, v)
+    assert bool(out[span[0]:].isnan().all()) and bool(lse[:, span[0]:].isnan().all())
+    assert not bool(out[:span[0]].isnan().any()) and not bool(lse[:, :span[0]].isnan().any())
 
 
 def test_every_output_is_optional_and_repeatable():
