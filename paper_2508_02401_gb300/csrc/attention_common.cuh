@@ -38,6 +38,7 @@ struct alignas(128) AttnParams {
     int G, hp, tp, nhb;  // heads of a KV group; heads and tokens of a row tile; head blocks of a group
     int unit_cost;       // what a unit costs beside its key tiles, in key tiles
     int min_run;         // length of a CTA's run, at least
+    int whole_tiles;     // units of up to so many key tiles are not cut
     float join_cost;     // what the join of a unit's part costs, in key tiles (0: nothing to speak of)
     int page_shift;
     float c;             // scale * log2(e)
@@ -319,6 +320,10 @@ struct Walk {
         t0 = static_cast<int>(off - static_cast<long long>(hb) * cost);
         at = r.w0 + max(0, p.unit_cost - t0);
         t0 = max(0, t0 - p.unit_cost);
+        if (t0 > 0 && kt <= p.whole_tiles) {  // another CTA's
+            at += kt - t0 + p.unit_cost;
+            t0 = kt;
+        }
     }
 
     // Item::n is left to the kernel.
@@ -344,7 +349,7 @@ struct Walk {
             I.part = kEndItem;
             return false;
         }
-        const int t1 = static_cast<int>(min(static_cast<long long>(kt), t0 + (r.w1 - at)));
+        const int t1 = kt <= p.whole_tiles ? kt : static_cast<int>(min(static_cast<long long>(kt), t0 + (r.w1 - at)));
         const int g = p.nhb == 1 ? hb : hb / p.nhb, b = hb - g * p.nhb;
         I.ntok = min(tq, q.n - j * tq);
         I.q_row = q.row0 + j * tq;

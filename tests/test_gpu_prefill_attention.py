@@ -95,6 +95,14 @@ def test_capped_grid(max_ctas):
           normal(T, 2, 128, seed=3))
 
 
+@pytest.mark.parametrize("max_ctas", [0, 3, 64])
+@pytest.mark.parametrize("lens", [(1000,), (1024, 1025, 1000), (900, 40, 1300, 2, 1151, 1153, 640, 1)])
+def test_prompts_about_the_length_of_uncut_units(lens, max_ctas):
+    """Row tiles of up to eight key tiles are whole, those above are cut, in runs that begin and end inside them."""
+    T = sum(lens)
+    check(config(8, 2, max_ctas=max_ctas), lens, normal(T, 8, 128, seed=1), normal(T, 2, 128, seed=2), normal(T, 2, 128, seed=3))
+
+
 def test_many_prompts():
     """More sequences than the plan has threads, empty ones among them."""
     lens = tuple(int(x) for x in np.random.default_rng(3).integers(0, 9, 900))
