@@ -466,7 +466,7 @@ typedef struct ckv_paged_cache {
  *   slot_map   [num_slots] out: the new tokens' slots, row after row; -1 behind the last one
  *   cu_new     [num_rows+1] out: first new token of each row
  *   lens_out, pool_out     out: the new lengths and counters; may be cache_lens and pool themselves
- * All device memory, not overlapping otherwise.  If the new tokens do not fit (a length is negative,
+ * All device memory, not overlapping otherwise (that is refused).  If the new tokens do not fit (a length is negative,
  * new_lens below -1, a row longer than max_blocks pages, more tokens than num_slots, too few free
  * pages, counters out of order), nothing is taken or given back: cu_new is 0, slot_map -1, lengths and
  * counters stay, and the status word gets code 5 with detail 1 (a row), 2 (num_slots), 3 (counters) or

@@ -573,6 +573,7 @@ def ckv_prefill_attention(cfg, batch, q, k, v, out, workspace, lse=None, lse_win
     take) are written where given."""
     dev, stream = _here(stream)
     T, hq, hkv = batch.total_tokens, cfg.num_q_heads, cfg.num_kv_heads
+    _packed("cu_seqlens", batch.cu_dev, _t.int32, dev, batch.num_seqs + 1)
     rc = (_lib or load()).ckv_prefill_attention(
         cfg.ref, batch.ref, _rows("q", q, dev, T, hq, q_tok_stride, q_head_stride), q_tok_stride, q_head_stride,
         _rows("k", k, dev, T, hkv, tok_stride, head_stride), _rows("v", v, dev, T, hkv, tok_stride, head_stride),

@@ -1877,6 +1877,31 @@ ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* 
         if (!aligned(p, 4)) return fail(CKV_ERR_INVALID_ARG, "an int32 array is not 4-byte aligned");
     if (!aligned(pool, 8) || !aligned(pool_out, 8))
         return fail(CKV_ERR_INVALID_ARG, "pool or pool_out is not 8-byte aligned");
+    // The kernel reads the lengths again after it has written: nothing that it writes may lie over anything else,
+    // but for the lengths and counters that are updated in place.
+    const struct {
+        const void* p;
+        int64_t bytes;
+        bool written;
+    } arrays[] = {{cache_lens, 4ll * num_rows, false},
+                  {new_lens, 4ll * num_rows, false},
+                  {pool, 16, false},
+                  {free_pages, 4ll * num_pages, true},
+                  {block_table, 4ll * num_rows * max_blocks, true},
+                  {slot_map, 4ll * num_slots, true},
+                  {cu_new, 4ll * (static_cast<int64_t>(num_rows) + 1), true},
+                  {lens_out, 4ll * num_rows, true},
+                  {pool_out, 16, true}};
+    constexpr int kLens = 0, kPool = 2, kLensOut = 7, kPoolOut = 8, kArrays = 9;
+    for (int i = 0; i < kArrays; ++i)
+        for (int j = 0; j < kArrays; ++j) {
+            const auto &x = arrays[i], &y = arrays[j];
+            if (i == j || !x.written) continue;
+            if (x.p == y.p && ((i == kLensOut && j == kLens) || (i == kPoolOut && j == kPool))) continue;
+            const uintptr_t u = reinterpret_cast<uintptr_t>(x.p), v = reinterpret_cast<uintptr_t>(y.p);
+            if (u < v + static_cast<uintptr_t>(y.bytes) && v < u + static_cast<uintptr_t>(x.bytes))
+                return fail(CKV_ERR_INVALID_ARG, "two of the arrays overlap");
+        }
     AttnWs l;
     ckv_status st = check_attn_ws(workspace, workspace_bytes, &l);
     if (st) return st;

@@ -38,8 +38,8 @@ def _paged(lib, cfg=None, cache=None, S=2, T=2, table=_P, blocks=4, lens=_P, cu=
                                    lse, lse_st, ws, ws_bytes, None)
 
 
-def _tables(lib, page=16, rows=2, lens=_P, new=_P, ring=_P, pages=10, pool=_P, table=_P, blocks=4, slots=_P, cap=5,
-            cu=_P, lens_out=_P, pool_out=_P, ws=_P, ws_bytes=_WS):
+def _tables(lib, page=16, rows=2, lens=_P, new=_P + 64, ring=_P + 128, pages=10, pool=_P + 192, table=_P + 256, blocks=4,
+            slots=_P + 320, cap=5, cu=_P + 384, lens_out=_P, pool_out=_P + 192, ws=_P + 1024, ws_bytes=_WS):
     return lib.ckv_block_tables(page, rows, lens, new, ring, pages, pool, table, blocks, slots, cap, cu, lens_out,
                                 pool_out, ws, ws_bytes, None)
 
@@ -103,6 +103,15 @@ def test_cache_arguments(lib, cache, expect):
 ])
 def test_block_tables_arguments(lib, kw, expect):
     assert _tables(lib, **kw) == expect
+
+
+@pytest.mark.parametrize("kw", [
+    dict(new=_P), dict(cu=_P), dict(cu=_P + 68), dict(slots=_P + 124), dict(table=_P + 204), dict(ring=_P + 256),
+    dict(lens_out=_P + 64), dict(lens_out=_P + 4), dict(pool_out=_P + 200), dict(pool_out=_P), dict(cu=_P + 320),
+    dict(lens_out=_P + 60), dict(table=_P + 300),
+])
+def test_block_tables_arrays_do_not_overlap(lib, kw):
+    assert _tables(lib, **kw) == 1
 
 
 @pytest.mark.parametrize("kw,expect", [

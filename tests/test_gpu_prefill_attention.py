@@ -286,7 +286,9 @@ def test_refusals():
     for bad in (dict(q=q.float()), dict(k=k.cpu()), dict(v=v[:, :1]), dict(out=out[:-1]), dict(q=q[::2]),
                 dict(q=q[:-1]), dict(lse=torch.empty(8, T - 1, device="cuda")),
                 dict(lse_win=torch.empty(8, 32, dtype=torch.float64, device="cuda")), dict(k=k[:, :, :64]),
-                dict(tok_stride=512), dict(out=out.transpose(0, 1))):
+                dict(tok_stride=512), dict(out=out.transpose(0, 1)), dict(batch=ckv.Batch([0, T], device="cpu")),
+                dict(batch=ckv.Batch([0, T], cu_seqlens_dev=batch.cu_dev.long())),
+                dict(batch=ckv.Batch([0, T], cu_seqlens_dev=batch.cu_dev[:1]))):
         with pytest.raises(ValueError):
             call(**bad)
     with pytest.raises(ckv.CkvError):
