@@ -493,6 +493,8 @@ CKV_API ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache*
  * call can be replayed as they grow.
  *   q, out [num_tokens, H_q, 128], lse [H_q][lse_head_stride] (stride >= num_tokens) as for
  *   ckv_prefill_attention.  Rows from cu_new[num_seqs] - cu_new[0] on (padding) are left as they were.
+ * num_tokens against num_seqs tells the call what to expect: up to twice as many are taken for single tokens,
+ * and long chunks among them (many of the sequences idle) are slow; leave idle sequences out of such a call.
  * Status code 3: cu_new that decreases or runs past num_tokens (then nothing is written); a sequence
  * with L < n or L beyond its table row (its rows are not written), or with a page outside the cache
  * (its rows are undefined). */

@@ -1706,8 +1706,12 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // Over a cache, the kernel for few rows where the sequences have at most 16 (token, head) rows of a KV head on
     // average.  8 sequences of 8000 cached tokens, 4 heads a group, few / tiles, us: 4 rows 47 / 56, 8 rows 52.2 / 57.1,
     // 12 rows 55.7 / 58.3, 16 rows 58.8 / 57.4; 1 sequence 19.8 / 29.6, 24.4 / 31.9 and 28.9 / 29.7 at 8, 12 and 16.
-    const int64_t rows = (static_cast<int64_t>(L.T) + L.S - 1) / L.S * (L.Hq / L.Hkv);
-    const bool few = L.paged && rows <= 16;
+    // Not where one of them may have many more (the lengths are on the device): 256 caches of 1000 tokens and a chunk
+    // of 512 over 8000 508 / 298.  Up to twice as many tokens as sequences count as single tokens: 256 caches of 300
+    // with 2 each 73 / 106, which costs a chunk among as many single ones (64 and 64: 130 / 88) and most of all one
+    // among idle sequences (256 tokens, 255 idle: 692 / 47).
+    const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
+    const bool few = L.paged && rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64);
     CUtensorMap mq, mk, mv;
     ckv_status st;
     if (!few) {

@@ -122,6 +122,14 @@ def test_nan_keys_in_one_part(new):
     assert not bool(out[new:].isnan().any()) and not bool(lse[:, new:].isnan().any())
 
 
+@pytest.mark.parametrize("singles", [0, 1])
+@pytest.mark.parametrize("chunk", [1, 17, 40, 41, 42, 130, 300])
+def test_a_chunk_among_single_tokens(chunk, singles):
+    """Either kernel takes single tokens (or idle sequences) and a chunk in one call."""
+    lens, new = [33 + 7 * i for i in range(40)] + [900], [singles] * 40 + [chunk]
+    Paged(config(8, 2), lens, new, 32, seed=19).check()
+
+
 def test_many_sequences():
     """More sequences than the plan has threads, empty ones among them."""
     g = np.random.default_rng(3)
