@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         *abort = 0;
         for (int i = 0; i < kRingT; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&freed[i], 1);
+            mbar_init(&freed[i], 2);  // the MMA issuers
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
@@ -195,24 +195,25 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         auto slot_of = [&](uint32_t d) { return cs + d >= kRingT ? cs + d - kRingT : cs + d; };  // d after the current K
         auto phase_of = [&](uint32_t d) { return cs + d >= kRingT ? cph ^ 1 : cph; };
         // One turn: the product of the current tile (`do_pv`; of its V, `valid` rows are the sequence's) and the logits
-        // of one (`do_qk`; K at ring position kd, with an item's first tile also its query rows).
-        auto play = [&](bool do_pv, bool first_v, bool last_v, bool free_v, int valid, bool clear, bool do_qk, uint32_t kd,
-                        bool first_q, bool last_q, bool free_k) {
+        // of one (`do_qk`; K at ring position kd, with an item's first tile also its query rows).  `has_v`, `has_k`: there are
+        // such tiles, whether or not this warpgroup has a part in them.  Both issuers release every tile: a commit
+        // covers only the MMAs of its own thread.  One without a part in a tile arrives plainly, after it has seen the tile
+        // in the ring too: the slot's release before that load is then complete, so it never arrives twice in one.
+        auto play = [&](bool do_pv, bool first_v, bool last_v, bool has_v, int valid, bool clear, bool do_qk, uint32_t kd,
+                        bool first_q, bool last_q, bool has_k) {
             const uint32_t ks = slot_of(kd), vs = slot_of(1);
             // (uniform registers)
             const uint32_t q_lo = uniform((q_addr + X * kTileUnits) | kDescLoK);
             const uint32_t k_lo = uniform((ring_addr + ks * kTileUnits) | kDescLoK);
             const uint32_t v_lo = uniform((ring_addr + vs * kTileUnits) | kDescLoV);
             const uint32_t accumulate = uniform(first_v ? 0 : 1);
-            if (do_qk) {
-                if (first_q) {
-                    if (!warp_wait(&q_full[X], qn & 1, abort, lim)) return false;
-                    ++qn;
-                }
-                tile_wait(&full[ks], phase_of(kd), abort, lim, a.status);
+            if (do_qk && first_q) {
+                if (!warp_wait(&q_full[X], qn & 1, abort, lim)) return false;
+                ++qn;
             }
+            if (has_k) tile_wait(&full[ks], phase_of(kd), abort, lim, a.status);
+            if (has_v) tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
             if (do_pv) {
-                tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
                 if (valid < kTileKeys && clear) clear_rows(ring + vs * kTileBytes, valid, lane);
                 tile_wait(&p_full[X], pn & 1, abort, lim, a.status);
                 ++pn;
@@ -239,9 +240,12 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                     }
                     umma_commit(&s_full[X]);
                 }
+                tc_fence_before_sync();
                 mbar_arrive(&turn[X ^ 1]);
-                if (do_pv && free_v) umma_commit(&freed[vs]);
-                if (do_qk && free_k) umma_commit(&freed[ks]);
+                if (do_pv) umma_commit(&freed[vs]);
+                else if (has_v) mbar_arrive(&freed[vs]);
+                if (do_qk) umma_commit(&freed[ks]);
+                else if (has_k) mbar_arrive(&freed[ks]);
                 if (do_qk && last_q) umma_commit(&q_free[X]);
             }
             __syncwarp();
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         ok = fetch();
         if (ok && !end_) {  // the first item's first logits
             const int n = X ? n1_ : n0_;
-            ok = play(false, false, false, false, 0, false, n > 0, 0, true, n == 1, X == 1 || n1_ == 0);
+            ok = play(false, false, false, false, 0, false, n > 0, 0, true, n == 1, true);
         }
         while (ok && !end_) {
             const int n0 = n0_, n1 = n1_, keys = keys_, n = X ? n1 : n0, rounds = max(n0, n1);
@@ -259,9 +263,8 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 if (last && !(ok = fetch())) break;
                 const int n_ = X ? n1_ : n0_;
                 const bool more = i + 1 < n, begin = last && !end_ && n_ > 0;
-                // A tile is freed by its last user: warpgroup 1 where it has a part in it.
-                ok = play(i < n, i == 0, i == n - 1, X == 1 || i >= n1, keys - i * kTileKeys, X == 0 || i >= n0, more || begin, 2,
-                          begin, begin ? n_ == 1 : i + 2 == n, X == 1 || (begin ? n1_ == 0 : i + 1 >= n1));
+                ok = play(i < n, i == 0, i == n - 1, true, keys - i * kTileKeys, X == 0 || i >= n0, more || begin, 2, begin,
+                          begin ? n_ == 1 : i + 2 == n, !last || !end_);
                 cph = phase_of(2);
                 cs = slot_of(2);
             }

@@ -130,6 +130,17 @@ def test_a_chunk_among_single_tokens(chunk, singles):
     Paged(config(8, 2), lens, new, 32, seed=19).check()
 
 
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (28, 4)])
+@pytest.mark.parametrize("max_ctas", [0, 1, 5])
+def test_key_tiles_of_one_row_tile(hq, hkv, max_ctas):
+    """Chunks whose units' first row tile sees fewer key tiles than the second, and units that have one row tile."""
+    c = Paged(config(hq, hkv, max_ctas=max_ctas), (1500, 300, 2700, 129, 640), (257, 3, 300, 129, 100), 16, seed=23)
+    out, lse = c.check()
+    for _ in range(10):
+        again = c.run()
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
 def test_many_sequences():
     """More sequences than the plan has threads, empty ones among them."""
     g = np.random.default_rng(3)

@@ -117,6 +117,21 @@ def test_one_long_prompt_per_cta_split():
           normal(6001, 1, 128, seed=3))
 
 
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (8, 2), (28, 4)])
+@pytest.mark.parametrize("max_ctas", [0, 1, 5])
+def test_key_tiles_of_one_row_tile(hq, hkv, max_ctas):
+    """A unit's first row tile does not see its last keys, short units have no second one, and parts of cut units
+    may have no tile for either: every tile of the ring is released once by both, call after call."""
+    lens = (100, 257, 1500, 128, 40, 2700, 129, 1, 1900)
+    T = sum(lens)
+    cfg = config(hq, hkv, max_ctas=max_ctas)
+    q, k, v = normal(T, hq, 128, seed=1), normal(T, hkv, 128, seed=2), normal(T, hkv, 128, seed=3)
+    out, lse, _ = check(cfg, lens, q, k, v)
+    for _ in range(10):
+        again = run(cfg, lens, q, k, v)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
 def test_strided_tensors():
     """q, k and v as slices of one fused projection [T, H_q + 2 H_kv, 128], and k, v interleaved."""
     hq, hkv, lens = 8, 2, (300, 77)
