@@ -110,12 +110,14 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
 // The waits for a tile, several in a row on the path from one product to the next, where a vote costs 1% and more.
 // One that gives up (or finds that another has) returns like the others: what follows works on whatever the
 // buffers hold, at addresses that are valid all the same, and the roles leave at their next item, whose waits
-// are agreed on.
-__device__ __forceinline__ void tile_wait(uint64_t* bar, uint32_t parity, volatile int* abort, long long lim, int* status) {
-    if (!mbar_wait(bar, parity, abort, lim)) {
-        *abort = 1;
-        record_error(status, kDevTimeout, 45);
-    }
+// are agreed on.  The result is for the MMA issuers: after a wait that gave up, a later one on the same barrier can take
+// the phase before for its own, so from then on they release no tile, and the loader never loads over one that is still on its
+// way.
+__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, volatile int* abort, long long lim, int* status) {
+    if (mbar_wait(bar, parity, abort, lim)) return true;
+    *abort = 1;
+    record_error(status, kDevTimeout, 45);
+    return false;
 }
 
 // A value that all lanes hold, in a uniform register.
@@ -476,7 +478,7 @@ struct TileLoader {
         return true;
     }
 
-    // Lets every issued copy land (before the block may exit).
+    // Lets every issued copy land, before the block may exit: others' waits for them may have given up.
     __device__ void drain() {
         volatile int never = 0;
         for (uint32_t k = use > RING ? use - RING : 0; k < use; ++k) mbar_wait(&full[k % RING], (k / RING) & 1, &never);

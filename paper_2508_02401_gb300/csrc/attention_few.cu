@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
         if (!ok) {
             *abort = 1;
             if (lane == 0) record_error(a.status, kDevTimeout, 51);
-            tiles.drain();
         }
+        tiles.drain();
         __syncwarp();
     } else if (warp == kQWarpF) {
         // ---------------------------------------------------------------- query rows
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
         const uint32_t ring_addr = desc_addr(ring), q_addr = desc_addr(qbuf), p_lo = desc_addr(pbuf) | (1u << 16);
         uint32_t sn = 0, pn = 0, cs = 0, cph = 0;  // logits and products issued; ring slot and phase of the next K
         int it = 0, end_ = 0, n_ = 0, keys_ = 0;
-        bool ok = true;
+        bool ok = true, live = true;  // live (a lane's own): none of its waits for a tile gave up
         auto fetch = [&]() {
             const int slot = it % kAttnItemRing;
             if (!warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim)) return false;
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
             const uint32_t k_lo = uniform((ring_addr + ks * kTileUnits) | kDescLoK);
             const uint32_t q_lo = uniform((q_addr + qs * (kQBytesF >> 4)) | kDescLoK);
             const uint32_t d_tmem = uniform(tm_s + (sn & 1) * kN);
-            tile_wait(&full[ks], phase_of(d), abort, lim, a.status);
+            live &= tile_wait(&full[ks], phase_of(d), abort, lim, a.status);
             __syncwarp();
             tc_fence_after_sync();
             if (elect_one()) {
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                     umma_ss<kDescHi>(d_tmem, k_lo + (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2,
                                      q_lo + (kk >> 2) * (kN * 128 >> 4) + (kk & 3) * 2, kIdescS, kk > 0 ? 1u : 0u);
                 umma_commit(&s_full[sn & 1]);
-                umma_commit(&freed[ks]);
+                if (live) umma_commit(&freed[ks]);
                 if (last) umma_commit(&q_free[qs]);
             }
             __syncwarp();
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                 const uint32_t vs = slot_of(1);
                 const uint32_t v_lo = uniform((ring_addr + vs * kTileUnits) | kDescLoV), d_tmem = uniform(tm_o);
                 const uint32_t accumulate = uniform(i > 0);
-                tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
+                live &= tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
                 if (keys - i * kTileKeys < kTileKeys) clear_rows(ring + vs * kTileBytes, keys - i * kTileKeys, lane);
                 tile_wait(p_full, pn & 1, abort, lim, a.status);
                 ++pn;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                         umma_ss<kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * kPGroup >> 4), kIdescO,
                                          kk > 0 ? 1u : accumulate);
                     umma_commit(pv_done);
-                    umma_commit(&freed[vs]);
+                    if (live) umma_commit(&freed[vs]);
                 }
                 __syncwarp();
                 if (last && !end_) ok = qk(2, true, n_ == 1);

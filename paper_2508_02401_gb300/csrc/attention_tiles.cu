@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         uint32_t qn = 0, pn = 0, turns = 0;         // items, tiles and turns of this one
         uint32_t cs = 0, cph = 0;                   // ring slot and phase of the current tile's K
         int it = 0;
-        bool ok = true;
+        bool ok = true, live = true;  // live (a lane's own): none of its waits for a tile gave up
         auto fetch = [&]() {
             const int slot = it % kAttnItemRing;
             if (!warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim)) return false;
@@ -211,8 +211,8 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 if (!warp_wait(&q_full[X], qn & 1, abort, lim)) return false;
                 ++qn;
             }
-            if (has_k) tile_wait(&full[ks], phase_of(kd), abort, lim, a.status);
-            if (has_v) tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
+            if (has_k) live &= tile_wait(&full[ks], phase_of(kd), abort, lim, a.status);
+            if (has_v) live &= tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
             if (do_pv) {
                 if (valid < kTileKeys && clear) clear_rows(ring + vs * kTileBytes, valid, lane);
                 tile_wait(&p_full[X], pn & 1, abort, lim, a.status);
@@ -242,10 +242,12 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 }
                 tc_fence_before_sync();
                 mbar_arrive(&turn[X ^ 1]);
-                if (do_pv) umma_commit(&freed[vs]);
-                else if (has_v) mbar_arrive(&freed[vs]);
-                if (do_qk) umma_commit(&freed[ks]);
-                else if (has_k) mbar_arrive(&freed[ks]);
+                if (live) {
+                    if (do_pv) umma_commit(&freed[vs]);
+                    else if (has_v) mbar_arrive(&freed[vs]);
+                    if (do_qk) umma_commit(&freed[ks]);
+                    else if (has_k) mbar_arrive(&freed[ks]);
+                }
                 if (do_qk && last_q) umma_commit(&q_free[X]);
             }
             __syncwarp();
@@ -326,11 +328,11 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
             if (!ok) {
                 *abort = 1;
                 if (lane == 0) record_error(a.status, kDevTimeout, 41);
-                volatile int never = 0;
-                tiles.drain();
-                if (qn0 > 0) mbar_wait(&q_full[0], (qn0 - 1) & 1, &never);
-                if (qn1 > 0) mbar_wait(&q_full[1], (qn1 - 1) & 1, &never);
             }
+            volatile int never = 0;
+            tiles.drain();
+            if (qn0 > 0) mbar_wait(&q_full[0], (qn0 - 1) & 1, &never);
+            if (qn1 > 0) mbar_wait(&q_full[1], (qn1 - 1) & 1, &never);
             __syncwarp();
         } else if (warp < kLoadWarp) {
             if (warp == kMmaWarp) mma_role(std::integral_constant<int, 0>{});
