@@ -246,7 +246,9 @@ __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads,
         r.W += scan[i];
         units += scan_units[i];
     }
-    if (bad && blockIdx.x == 0 && threadIdx.x == 0) record_error(a.status, kDevBadIndex, -1);
+    // The host's copy of a batch is in order and has tokens (a call without any is not launched): no need of its hash.
+    if ((bad || (r.W == 0 && a.check_hash)) && blockIdx.x == 0 && threadIdx.x == 0)
+        record_error(a.status, a.check_hash ? kDevBadSeqlens : kDevBadIndex, -1);
     if (bad || r.W == 0) return false;
     // A unit of k tiles in runs of r of them takes r and its k / r parts' joins: least at r = sqrt(k join_cost).
     int least = p.min_run;

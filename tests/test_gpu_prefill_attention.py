@@ -289,6 +289,20 @@ def test_lengths_on_the_device_that_disagree_are_reported():
     out.check()
 
 
+@pytest.mark.parametrize("dev", [(0, 0, 0, 0), (7, 7, 7, 7), (0, 150, 100, 200), (0, 100, 100, 5000), (-3, 100, 150, 200),
+                                 (0, 200, 100, 200)])
+def test_device_lengths_without_tokens_or_out_of_order_are_reported(dev):
+    """A copy that is not there yet (no token at all) or that makes no sense: code 1 and nothing written."""
+    cfg, T = config(), 200
+    q, k, v = normal(T, 8, 128, seed=1), normal(T, 2, 128, seed=2), normal(T, 2, 128, seed=3)
+    ws, out = ckv.new_attention_workspace(cfg), Guarded((T, 8, 128), torch.bfloat16, 7.0)
+    batch = ckv.Batch([0, 100, 150, T], cu_seqlens_dev=torch.tensor(dev, dtype=torch.int32, device="cuda"))
+    ckv.ckv_prefill_attention(cfg, batch, q, k, v, out.view, ws)
+    assert ckv.ckv_read_device_status(ws)[0] == 1
+    out.check()
+    assert bool((out.view == 7).all())
+
+
 def test_refusals():
     cfg, T = config(), 64
     q, k, v = normal(T, 8, 128), normal(T, 2, 128), normal(T, 2, 128)
