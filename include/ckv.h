@@ -470,7 +470,8 @@ typedef struct ckv_paged_cache {
  * new_lens below -1, a row longer than max_blocks pages, more tokens than num_slots, too few free
  * pages, counters out of order), nothing is taken or given back: cu_new is 0, slot_map -1, lengths and
  * counters stay, and the status word gets code 5 with detail 1 (a row), 2 (num_slots), 3 (counters) or
- * 4 (pages).  A page index outside [0, num_pages) gives slot -1 and code 3. */
+ * 4 (pages).  A page index outside [0, num_pages) gives slot -1 and code 3, with detail the row; in a row that is given
+ * back, -1 goes into the ring in its place and the code is the same. */
 CKV_API ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* cache_lens,
                                     const int32_t* new_lens, int32_t* free_pages, int32_t num_pages,
                                     const int64_t* pool, int32_t* block_table, int32_t max_blocks,

@@ -165,8 +165,12 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const __grid_
                 at += c.give;
             }
             const long long to = give0 + x;
-            p.a.free_pages[to < cap_pages ? to : to - cap_pages] =
-                p.a.table[static_cast<size_t>(r) * p.a.max_blocks + (x - at)];
+            int page = p.a.table[static_cast<size_t>(r) * p.a.max_blocks + (x - at)];
+            if (page < 0 || page >= p.a.num_pages) {  // (its place in the ring is counted already)
+                record_error(p.a.status, kDevBadIndex, r);
+                page = -1;
+            }
+            p.a.free_pages[to < cap_pages ? to : to - cap_pages] = page;
         }
     }
     if (blockIdx.x == 0) {

@@ -156,6 +156,27 @@ def test_bad_lengths_counters_and_pages():
     assert code == 3 and not same and slots[:3].tolist() == [-1, 48, -1]
 
 
+def test_bad_pages_given_back():
+    """Table entries outside the cache are reported with their row when the row is given back, and -1 is in the ring in
+    their place."""
+    t = Tables(3, 10, 8, 16, seed=5)
+    d, ws = t.d, t.ws
+    slots, cu = torch.zeros(64, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    ring, pool, lens = dev([0, 0, 0, 0, 7, 8, 0, 0, 0, 0]), dev([4, 6], torch.int64), dev([16, 40, 0])
+    d["table"][0, 0] = 5
+    d["table"][1, :3] = dev([2, -1, 10])
+
+    def call(new):
+        ckv.ckv_block_tables(16, lens, dev(new), ring, pool, d["table"], slots, cu, lens, pool, ws)
+        return ckv.ckv_read_device_status(ws)
+
+    assert call([-1, -1, 1]) == (3, 1)
+    assert ring[4:].tolist() == [7, 8, 5, 2, -1, -1] and pool.tolist() == [5, 10] and lens.tolist() == [0, 0, 1]
+    assert slots[:2].tolist() == [7 * 16, -1]
+    assert call([48, 0, 15]) == (0, 0)  # pages 8, 5 and 2
+    assert call([0, 1, 0]) == (3, 1) and slots[:2].tolist() == [-1, -1]  # the first of the bad ones
+
+
 def test_tables_replayed_in_a_graph():
     """The step of a decode loop, captured once: lengths, counters and tables move on the device."""
     t = Tables(6, 200, 20, 16, seed=4)
