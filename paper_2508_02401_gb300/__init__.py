@@ -524,6 +524,8 @@ class PagedCache:
                 raise ValueError("k_pages and v_pages are [num_pages, page_size, H_kv, 128] of the same strides")
             if t.numel() and t.stride()[1:] != (t.shape[2] * 128, 128, 1):
                 raise ValueError(f"{name}: a page is not packed")
+            if t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2] * 128:
+                raise ValueError(f"{name}: the pages overlap (page stride {t.stride(0)})")
         if k_pages.device != v_pages.device:
             raise ValueError("k_pages and v_pages are on different devices")
         self.k_pages, self.v_pages = k_pages, v_pages

@@ -258,6 +258,17 @@ def test_refusals():
                                  a["lens"], a["pool"], ws)
 
 
+def test_pages_that_overlap_are_refused():
+    """Pages expanded over the first dimension, or less than a page apart: the rows that a call of such strides would
+    reach are not there."""
+    one = torch.zeros((1, 16, 2, 128), dtype=torch.bfloat16, device="cuda")
+    assert ckv.PagedCache(one, one.clone()).num_pages == 1
+    for pages in (one.expand(4, 16, 2, 128), one.as_strided((2, 8, 2, 128), (2048 - 256, 256, 128, 1)),
+                  one.as_strided((2, 8, 2, 128), (256, 256, 128, 1))):
+        with pytest.raises(ValueError, match="page"):
+            ckv.PagedCache(pages, pages)
+
+
 @pytest.mark.parametrize("hq,hkv,page,lens", [(8, 2, 16, (300, 40, 700)), (28, 4, 32, (513, 1000))])
 def test_prefill_compress_cache_decode(hq, hkv, page, lens):
     """Two layers of different budgets over one pool of pages: the prefill attention's window lse feeds
