@@ -450,13 +450,14 @@ ckv_status check_kv(const void* p, const char* name, int T) {
     return CKV_OK;
 }
 
-ckv_status resolve_strides(const Plan& pl, int64_t* tok, int64_t* head) {
-    if (*tok == 0) *tok = static_cast<int64_t>(pl.Hkv) * kHeadDim;
+// Strides of a [T, heads, 128] tensor: 0 = packed, else positive multiples of 8 elements (16 bytes).
+ckv_status check_strides(const char* name, int heads, int64_t* tok, int64_t* head) {
+    if (*tok == 0) *tok = static_cast<int64_t>(heads) * kHeadDim;
     if (*head == 0) *head = kHeadDim;
     if (*tok < 0 || *head < 0 || *tok % 8 || *head % 8)
-        return fail(CKV_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+        return fail(CKV_ERR_INVALID_ARG, "%s strides must be non-negative multiples of 8 elements", name);
     if (*tok >= (static_cast<int64_t>(1) << 38) || *head >= (static_cast<int64_t>(1) << 38))
-        return fail(CKV_ERR_UNSUPPORTED, "stride too large");
+        return fail(CKV_ERR_UNSUPPORTED, "%s stride too large", name);
     return CKV_OK;
 }
 
@@ -994,7 +995,7 @@ ckv_status score_window_impl(const ckv_config* cfg, int32_t layer, const ckv_bat
     if (st) return st;
     int T = 0;
     WsLayout l;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)) ||
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)) ||
         (st = check_kv(q_win, "q_win", T)) || (st = check_kv(k, "k", T)) ||
         (st = check_kv(scores, "scores", T)) ||
         (st = check_ws(pl, batch, T, workspace, workspace_bytes, &l)))
@@ -1076,7 +1077,7 @@ ckv_status ckv_gather_compact(const ckv_config* cfg, const ckv_batch* batch, int
     Plan pl;
     pl.Hkv = cfg->num_kv_heads;
     int T = 0;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)))
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)))
         return st;
     if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < sizeof(WsHeader))
         return fail(CKV_ERR_WORKSPACE, "workspace missing, misaligned or too small");
@@ -1166,7 +1167,7 @@ ckv_status compress_layer_impl(const ckv_config* cfg, int32_t layer, const ckv_b
     if (st) return st;
     int T = 0;
     WsLayout l;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)) ||
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)) ||
         (st = check_kv(q_win, "q_win", T)) || (st = check_kv(k, "k", T)) ||
         (st = check_kv(v, "v", T)) || (st = check_ws(pl, batch, T, workspace, workspace_bytes, &l)))
         return st;
@@ -1198,7 +1199,7 @@ ckv_status ckv_select_compact(const ckv_config* cfg, int32_t layer, const ckv_ba
     if (st) return st;
     int T = 0;
     WsLayout l;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)) ||
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)) ||
         (st = check_kv(k, "k", T)) || (st = check_kv(v, "v", T)) ||
         (st = check_ws(pl, batch, T, workspace, workspace_bytes, &l)))
         return st;
@@ -1304,7 +1305,7 @@ ckv_status layer_jobs(const std::vector<Plan>& pls, const ckv_layer_io* io, int 
     for (int i = 0; i < n; ++i) {
         tok[i] = io[i].tok_stride;
         head[i] = io[i].head_stride;
-        if ((st = resolve_strides(pls[i], &tok[i], &head[i])) || (st = check_kv(io[i].q_win, "q_win", T)) ||
+        if ((st = check_strides("k/v", pls[i].Hkv, &tok[i], &head[i])) || (st = check_kv(io[i].q_win, "q_win", T)) ||
             (st = check_kv(io[i].k, "k", T)))
             return st;
         if (pls[i].w != pls[0].w) return fail(CKV_ERR_INVALID_ARG, "layers with different windows");
@@ -1466,7 +1467,7 @@ ckv_status ckv_semantic_retrieval_scores(const ckv_config* cfg, int32_t layer, c
     if (st) return st;
     int T = 0;
     WsLayout l;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)) ||
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)) ||
         (st = check_kv(q_dec, "q_dec", T)) || (st = check_kv(k, "k", T)) ||
         (st = check_ws(pl, batch, T, workspace, workspace_bytes, &l)) ||
         (st = check_lse(pl, batch, lse, &lse_head_stride)))
@@ -1540,7 +1541,7 @@ ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer, const c
     ckv_status st = make_plan(cfg, layer, pl);
     if (st) return st;
     int T = 0;
-    if ((st = check_batch(batch, &T)) || (st = resolve_strides(pl, &tok_stride, &head_stride)) ||
+    if ((st = check_batch(batch, &T)) || (st = check_strides("k/v", pl.Hkv, &tok_stride, &head_stride)) ||
         (st = check_kv(q_win, "q_win", T)) || (st = check_kv(k, "k", T)) ||
         (st = check_kv(scores, "scores", T)))
         return st;
@@ -1632,17 +1633,6 @@ ckv_status check_attn_ws(void* ws, size_t bytes, AttnWs* l) {
     if (!aligned(ws, kWsAlign)) return fail(CKV_ERR_WORKSPACE, "workspace not 256-byte aligned");
     if (bytes < l->total)
         return fail(CKV_ERR_WORKSPACE, "workspace %zu bytes < required %zu", bytes, l->total);
-    return CKV_OK;
-}
-
-// Strides of a [T, heads, 128] tensor: 0 = packed, else positive multiples of 8 elements (16 bytes).
-ckv_status check_strides(const char* name, int heads, int64_t* tok, int64_t* head) {
-    if (*tok == 0) *tok = static_cast<int64_t>(heads) * kHeadDim;
-    if (*head == 0) *head = kHeadDim;
-    if (*tok < 0 || *head < 0 || *tok % 8 || *head % 8)
-        return fail(CKV_ERR_INVALID_ARG, "%s strides must be non-negative multiples of 8 elements", name);
-    if (*tok >= (static_cast<int64_t>(1) << 38) || *head >= (static_cast<int64_t>(1) << 38))
-        return fail(CKV_ERR_UNSUPPORTED, "%s stride too large", name);
     return CKV_OK;
 }
 
