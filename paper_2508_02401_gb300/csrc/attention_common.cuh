@@ -399,12 +399,14 @@ __device__ __forceinline__ bool last_part(const AttnLaunch& a, const Item& I) {
     return last;
 }
 
+// WINDOW: the call has the window rows' lse as an output (prompts).
+template <bool WINDOW>
 __device__ __forceinline__ void write_lse(const AttnLaunch& a, const Item& I, int tok, int head, float mc, float l) {
-    if (!a.lse && !a.lse_win) return;
+    if (!a.lse && !(WINDOW && a.lse_win)) return;
     const float lse = (mc + lg2_approx(l)) * 0.6931471805599453f;  // (2^-22 of absolute error in the logarithm)
     const int t = I.q_row + tok, h = I.head0 + head;
     if (a.lse) a.lse[h * a.lse_stride + t] = lse;
-    if (a.lse_win) {
+    if (WINDOW && a.lse_win) {
         const int rw = I.pos0 + tok - (I.len - a.w);
         if (rw >= 0) a.lse_win[h * a.lse_win_stride + static_cast<long long>(I.seq) * a.w + rw] = lse;
     }

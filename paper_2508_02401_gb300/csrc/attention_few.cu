@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const AttnLaunch& a = p.a;
-    const int heads = a.Hkv * p.nhb;    // units of a row tile
+    const int heads = a.Hkv;            // units of a row tile (a unit has whole KV groups of G = p.hp heads)
     if ((smem_u32(sm) & 1023u) != 0) {  // the swizzled tiles need an aligned base
         if (threadIdx.x == 0) record_error(a.status, kDevBadIndex, -2);
         return;
@@ -203,12 +203,12 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
             if (!(ok = warp_wait(&q_free[qs], ((it >> 1) & 1) ^ 1, abort, lim))) break;
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
             uint8_t* dst = qbuf + qs * kQBytesF;
-            const int chunks = I.ntok * p.hp * 16;
+            const int chunks = p.tp * p.hp * 16;
 #pragma unroll 4
             for (int x = lane; x < chunks; x += 32) {
                 const int r = x >> 4, ch = x & 15;
                 const int t = r / p.hp, h = r - t * p.hp;
-                if (h >= I.nheads) continue;
+                if (t >= I.ntok) continue;
                 const uint4 val = *reinterpret_cast<const uint4*>(
                     src + (I.q_row + t) * a.q_tok + (I.head0 + h) * a.q_head + ch * 8);
                 *reinterpret_cast<uint4*>(dst + (ch >> 3) * (kN * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
@@ -452,11 +452,10 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                     h = 0;
                     ++t;
                 }
-                if (h >= I.nheads) continue;
                 const float L = (red[x] + red[COLS + x]) + (red[2 * COLS + x] + red[3 * COLS + x]);
                 if (whole) {
                     out[(t * a.Hq + h) * kHeadDim] = __float2bfloat16(o[x] * (1.f / L));
-                    if (dim == 0) write_lse(a, I, t, h, ref[x], L);
+                    if (dim == 0) write_lse<false>(a, I, t, h, ref[x], L);
                 } else {
                     part[x * 128 + dim] = o[x];
                     if (dim == 0) {
@@ -477,7 +476,6 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
             // the row, four dims.
             for (int x = warp; x < rows; x += 4) {
                 const int tx = x / p.hp, hx = x - tx * p.hp;
-                if (hx >= I.nheads) continue;
                 float M = -INFINITY, L = 0.f;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int k0 = 0; k0 < I.n_parts; k0 += 32) {
@@ -517,7 +515,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                 __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
                                      (static_cast<long long>(I.q_row + tx) * a.Hq + I.head0 + hx) * kHeadDim + lane * 4;
                 *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (lane == 0) write_lse(a, I, tx, hx, M, L);
+                if (lane == 0) write_lse<false>(a, I, tx, hx, M, L);
             }
         }
         if (!ok) {
@@ -537,9 +535,9 @@ cudaError_t launch_few(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) 
     static bool configured[kAttnMaxDevices] = {};
     const cudaError_t e = attn_configure(kern, FewSmem::kBytes, configured);
     if (e != cudaSuccess) return e;
-    p.hp = attn_heads_per_tile(L.Hq, L.Hkv, COLS);
-    p.tp = COLS / p.hp;
-    p.nhb = (p.G + p.hp - 1) / p.hp;
+    p.hp = p.G;
+    p.tp = COLS / p.G;
+    p.nhb = 1;
     const int sms = device_sm_count();
     if (sms <= 0) return cudaErrorNoDevice;
     int grid = sms * kCtasF;

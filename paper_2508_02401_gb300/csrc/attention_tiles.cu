@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 }
             }
             if (whole) {
-                if (valid) write_lse(a, I, tok, h_r, mc, l);
+                if (valid) write_lse<!PAGED>(a, I, tok, h_r, mc, l);
                 continue;
             }
             if (valid) {
@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                     store_bf16(out + q4 + x, pk, wide);
                 }
             }
-            write_lse(a, I, tok, h_r, M, L);
+            write_lse<!PAGED>(a, I, tok, h_r, M, L);
         }
         if (!ok) {
             *abort = 1;
@@ -558,7 +558,7 @@ cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q
     p.tmap_v = map_v;
     p.a = L;
     p.G = L.Hq / L.Hkv;
-    p.hp = attn_heads_per_tile(L.Hq, L.Hkv, kTileKeys);
+    p.hp = attn_heads_per_tile(L.Hq, L.Hkv);
     p.tp = kTileKeys / p.hp;
     p.nhb = (p.G + p.hp - 1) / p.hp;
     p.unit_cost = 3;

@@ -1705,7 +1705,7 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     CUtensorMap mq, mk, mv;
     ckv_status st;
     if (!few) {
-        const int hp = attn_heads_per_tile(L.Hq, L.Hkv, kTileKeys), tp = kTileKeys / hp;
+        const int hp = attn_heads_per_tile(L.Hq, L.Hkv), tp = kTileKeys / hp;
         const int64_t dims[3] = {kHeadDim, L.Hq, L.T}, strides[3] = {1, L.q_head, L.q_tok};
         const int box[3] = {64, hp, tp};
         if ((st = make_rows_map(&mq, L.q, 3, dims, strides, box))) return st;

@@ -236,13 +236,13 @@ struct AttnLaunch {
     bool check_hash;                // cu has to hash to cu_hash
     uint32_t cu_hash;
 };
-// Query heads of a KV group that share a tile of `rows` (token, head) rows.
-constexpr int attn_heads_per_tile(int Hq, int Hkv, int rows) { return Hq / Hkv < rows ? Hq / Hkv : rows; }
+// Query heads of a KV group that share a tile of 128 (token, head) rows.
+constexpr int attn_heads_per_tile(int Hq, int Hkv) { return Hq / Hkv < 128 ? Hq / Hkv : 128; }
 // Two tiles of 128 rows a CTA (attention_tiles.cu).
 cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q, const CUtensorMap& map_k,
                                    const CUtensorMap& map_v, cudaStream_t stream);
 // Over a paged cache, units of 4, 8 or 16 rows: the least that takes `rows`, the rows that a sequence has on
-// average (attention_few.cu).
+// average (attention_few.cu): at least a token's H_q / H_kv, at most 16.
 cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, const CUtensorMap& map_v, int rows,
                                  cudaStream_t stream);
 
