@@ -230,6 +230,50 @@ def test_same_results_on_another_stream_and_again():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (8, 2)])
+@pytest.mark.parametrize("new", [3, 600])
+def test_values_that_are_not_finite_reach_no_row_far_before_them(hq, hkv, new):
+    """As in a prompt, from chunks that begin inside a tile."""
+    L = 1171
+    c = Paged(config(hq, hkv), (L, 300), (new, 1), 32, seed=24)
+    want = [x.clone() for x in c.run()]
+    for j in (L - 1, L - 300, L - 599):
+        at = int(c.table[0, j // 32]), j % 32
+        was = c.v_pages[at].clone()
+        c.v_pages[at] = math.nan
+        out, lse = c.run()
+        c.v_pages[at] = was
+        first = j - (L - new)  # the first query row that sees it
+        far = max(0, first - 255)
+        assert torch.equal(out[:far], want[0][:far]) and torch.equal(lse, want[1])
+        assert bool(out[max(0, first):new].isnan().all()) and torch.equal(out[new:], want[0][new:])
+
+
+def test_calls_of_both_kernels_at_once():
+    """Three streams, a workspace each: single tokens, chunks, and the next step's tables beside them."""
+    one, chunk = Paged(config(8, 2), (5000, 77, 300), (1, 1, 1), 32, seed=25), Paged(config(8, 2), (3000, 900), (300, 70), 32, seed=26)
+    calls = []
+    for c in (one, chunk):
+        out = torch.zeros_like(c.q)
+        calls.append((c, ckv.PagedCache(c.k_pages, c.v_pages), dev(c.table), dev(c.lens), dev(c.cu), out,
+                      ckv.new_attention_workspace(c.cfg), torch.cuda.Stream(), c.run()[0].clone()))
+    rows, pages = 500, 2000
+    lens, ring, pool = dev(np.zeros(rows)), dev(np.arange(pages)), dev([0, pages], torch.int64)
+    table, slots, cu = dev(np.zeros((rows, 4))), dev(np.zeros(rows)), dev(np.zeros(rows + 1))
+    new, ws, side = dev(np.ones(rows)), ckv.new_attention_workspace(one.cfg), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(60):
+        for c, cache, t, n, cn, out, w, stream, _ in calls:
+            ckv.ckv_paged_attention(c.cfg, cache, t, n, cn, c.q, out, w, stream=stream)
+        ckv.ckv_block_tables(16, lens, new, ring, pool, table, slots, cu, lens, pool, ws, stream=side)
+    torch.cuda.synchronize()
+    for c, _, _, _, _, out, w, _, want in calls:
+        assert torch.equal(out, want) and ckv.ckv_read_device_status(w) == (0, 0)
+    assert ckv.ckv_read_device_status(ws) == (0, 0)
+    assert bool((lens == 60).all()) and pool.tolist() == [2000, 2000]
+    assert sorted(table.reshape(-1).tolist()) == list(range(pages))
+
+
 @pytest.mark.parametrize("what", ["page", "negative", "short", "long", "decreasing", "past_the_end", "negative_cu"])
 def test_bad_lengths_and_pages_are_reported(what):
     """Other sequences' rows are right all the same; nothing outside the outputs is touched."""

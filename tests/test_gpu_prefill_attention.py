@@ -212,6 +212,21 @@ def test_masked_keys_of_any_value():
         assert torch.equal(got[0][:333], want[0][:333]) and torch.equal(got[1][:, :333], want[1][:, :333])
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (8, 2), (28, 4), (6, 2)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_that_are_not_finite_reach_no_row_far_before_them(hq, hkv, bad):
+    """A row at least 256 tokens before such a value is as if it were not there; every row that sees it is not finite."""
+    T = 1300
+    cfg, q, k, v = config(hq, hkv), normal(T, hq, 128, seed=1), normal(T, hkv, 128, seed=2), normal(T, hkv, 128, seed=3)
+    want = run(cfg, (T,), q, k, v)
+    for j in (256, 511, 700, 1023, 1299):
+        vv = v.clone()
+        vv[j] = bad
+        got = run(cfg, (T,), q, k, vv)
+        assert torch.equal(got[0][:j - 255], want[0][:j - 255]) and torch.equal(got[1], want[1])
+        assert not bool(got[0][j:].isfinite().any())
+
+
 @pytest.mark.parametrize("span", [(0, 1), (256, 640), (0, 4096), (4000, 4096)])
 def test_nan_keys_that_rows_see(span):
     """NaN keys, a tile's or a part's worth of them: every row that sees one is NaN, in out and lse."""
