@@ -410,7 +410,8 @@ CKV_API ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer,
  * ckv_block_tables -> ckv_cache_write -> ckv_paged_attention.  (The paper's own decoding over the
  * compressed cache is Eq. 3-4; its prefill attention is Eq. 2.)
  *
- * The workspace of these calls is ckv_attention_workspace_size's, zeroed once like the others, and again
+ * The workspace of these calls is ckv_attention_workspace_size's (one for all four; ckv_block_tables and
+ * ckv_cache_write touch only its first 1.5 KB, and ask for the whole of it all the same), zeroed once like the others, and again
  * after a status of code 2 (a wait that gave up can leave the count of a unit's parts open); the rules
  * above for workspaces, streams, alignment and errors hold.  Of the config they read the head
  * counts, window, softmax_scale and max_ctas.  fp32 logits, sums and outputs' accumulation; the
@@ -495,7 +496,8 @@ CKV_API ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache*
  *   q, out [num_tokens, H_q, 128], lse [H_q][lse_head_stride] (stride >= num_tokens) as for
  *   ckv_prefill_attention.  Rows from cu_new[num_seqs] - cu_new[0] on (padding) are left as they were.
  * num_tokens against num_seqs tells the call what to expect: up to twice as many are taken for single tokens,
- * and long chunks among them (many of the sequences idle) are slow; leave idle sequences out of such a call.
+ * and long chunks among them (many of the sequences idle) are slow; leave idle sequences out of such a call.  Padding
+ * rows count as tokens there, so a few of them can move a small call of single tokens to the slower side.
  * Status code 3: cu_new that decreases or runs past num_tokens (then nothing is written); a sequence
  * with L < n or L beyond its table row (its rows are not written), or with a page outside the cache
  * (its rows are undefined). */

@@ -6,8 +6,10 @@
 //
 // One pass over the keys in tiles of 128 (the online softmax): with a reference m of the row's logits,
 // l = sum 2^(x_j - m) and o = sum 2^(x_j - m) v_j; when a tile's maximum passes m by more than 2^8, m
-// moves there and l and o are multiplied by 2^(m_old - m_new).  A smaller excess is left: numerators up
-// to 2^8 cost no precision, and the reference then hardly ever moves after a row's first tile.
+// moves there and l and o are multiplied by 2^(m_old - m_new).  A smaller excess is left (a published refinement of
+// the online softmax): numerators up to 2^8 cost no precision, and the reference then hardly ever moves after a row's
+// first tile.  The numerators are rounded to bf16 for the product with v (2^-8 of each at most): the tensor core takes two
+// operands of one type, and v is bf16.  Their sum l takes them as they were, in 32 bits.
 //
 // A unit is (sequence, row tile, block of a KV head's query heads); its rows are (token, head) pairs,
 // token major, so that the heads that share keys share the tile.  The units stand in order on a line, each
@@ -134,7 +136,8 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int valid, int lane) {
 }
 
 // ---------------------------------------------------------------------------- the plan
-// Sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm on (a, m).
+// Sum over i < n of floor((a i + b) / m), by the steps of Euclid's algorithm on (a, m): the known recursion for sums
+// of floors, which swaps the two after each division.
 __device__ inline unsigned long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a,
                                                unsigned long long b) {
     unsigned long long s = 0;

@@ -7,7 +7,7 @@
 //
 // Bound by the loads of K and V: 64 KB a key tile, 1.5 us of an SM's share of the bandwidth (8 caches of 131072
 // tokens, 4.3 GB: 620 us, 6.9 TB/s).  Two CTAs run on an SM, so that one's start and end of a unit lie beside the
-// other's loads; what they do not hide shows on short caches (256 of 300 tokens, 319 MB: 62 us).
+// other's loads; what they do not hide shows on short caches (256 of 300 tokens, 319 MB: 61 us).
 #include "attention_common.cuh"
 
 namespace ckv {
@@ -565,7 +565,8 @@ cudaError_t launch_attention_few(const AttnLaunch& L, const CUtensorMap& map_k, 
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
     p.wait_cycles = wait_limit_cycles();
-    // Only the columns in use are worked on: 256 caches of 300 tokens, 4 rows each, 61.9 us with 4 columns, 67.1 with 16.
+    // Only the columns in use are worked on: 256 caches of 300 tokens, 4 rows each, 61.9 us with 4 columns, 67.1 with 16
+    // (when it was measured; 61 now).
     return rows <= 4 ? launch_few<4>(L, p, stream) : rows <= 8 ? launch_few<8>(L, p, stream) : launch_few<16>(L, p, stream);
 }
 

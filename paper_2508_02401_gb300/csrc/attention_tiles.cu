@@ -7,8 +7,8 @@
 //
 // Bound by the power limit and, before it, by the path from one product to the next.  A key tile takes
 // the tensor core 2048 cycles (four products of 128 x 128 x 128, 512 each, the rate that MMAs issued back to back
-// reach).  One prompt of 32768 tokens (32 / 8 heads): 1500 TFLOP/s at 1375 W and 1650 MHz, where the tensor core is at
-// work 75% of the time; without its loads (a copy that skipped them) 1820.
+// reach).  One prompt of 32768 tokens (32 / 8 heads): 1475 TFLOP/s at 1375 W and 1670 MHz, where the tensor core is at
+// work 72% of the time; without its loads (a copy that skipped them) 1820.
 #include <type_traits>
 
 #include "attention_common.cuh"
@@ -166,8 +166,10 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
     // S = Q K^T and O += P V of warpgroup X.  The two take turns: the tensor core holds up an issue of eight MMAs until
     // some 200 cycles before it is done with them, and with one issuer for both, its waits between the products
     // (about 560 cycles for each) left the tensor core idle; without turns the warpgroups' products interleave and finish
-    // together, with nothing to overlap the softmaxes (one prompt of 8192 tokens: 374 us with one issuer, 436
-    // without turns, 367 so).  An issuer waits for its tiles while the other issues.
+    // together, with nothing to overlap the softmaxes (one prompt of 8192 tokens, on one box: 374 us with one issuer, 436
+    // without turns, 367 so; 370 to 400 by box).  An issuer waits for its tiles while the other issues.
+    // The next logits go over the numerators of the tile before: their MMAs follow, from the same thread, those of the
+    // product that reads them, and the tensor core takes one thread's MMAs in the order of their issue.
     // A turn is the product of a tile and then the logits of the warpgroup's next (or of its next unit's first):
     // its softmax runs in the other's turn.
     auto mma_role = [&](auto xc) {
@@ -563,8 +565,8 @@ cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q
     p.nhb = (p.G + p.hp - 1) / p.hp;
     p.unit_cost = 3;
     p.min_run = 4;
-    // 1000 tokens (32/8 heads) 31.9 us with 4, 23.9 with 8; 8 x 1000 98.7 and 89.4; 2048 tokens 48.7 with 4 and 8,
-    // 57.7 with 16.
+    // 1000 tokens (32/8 heads) 31.9 us with 4, 23.9 with 8; 8 x 1000 98.7 and 89.4 (92 on other boxes); 2048 tokens 48.7
+    // with 4 and 8, 57.7 with 16.
     p.whole_tiles = 8;
     p.join_cost = 1.f;
     p.page_shift = 0;

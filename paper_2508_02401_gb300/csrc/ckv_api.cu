@@ -1694,12 +1694,12 @@ ckv_status make_rows_map(CUtensorMap* map, const void* ptr, int rank, const int6
 
 ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // Over a cache, the kernel for few rows where the sequences have at most 16 (token, head) rows of a KV head on
-    // average.  8 sequences of 8000 cached tokens, 4 heads a group, few / tiles, us: 4 rows 47 / 56, 8 rows 52.2 / 57.1,
-    // 12 rows 55.7 / 58.3, 16 rows 58.8 / 57.4; 1 sequence 19.8 / 29.6, 24.4 / 31.9 and 28.9 / 29.7 at 8, 12 and 16.
+    // average.  8 sequences of 8000 cached tokens, 4 heads a group, few / tiles, us: 4 rows 49.2 / 58.9, 8 rows 51.8 / 58.2,
+    // 12 rows 54.8 / 58.9, 16 rows 58.2 / 58.3; 1 sequence 15.8 / 31.6, 20.4 / 30.2, 24.9 / 31.8 and 29.0 / 30.2.
     // Not where one of them may have many more (the lengths are on the device): 256 caches of 1000 tokens and a chunk
-    // of 512 over 8000 508 / 298.  Up to twice as many tokens as sequences count as single tokens: 256 caches of 300
-    // with 2 each 73 / 106, which costs a chunk among as many single ones (64 and 64: 130 / 88) and most of all one
-    // among idle sequences (256 tokens, 255 idle: 692 / 47).
+    // of 512 over 8000 511 / 300.  Up to twice as many tokens as sequences count as single tokens: 256 caches of 300
+    // with 2 each 69.4 / 110, which costs a chunk among as many single ones (64 and 64: 131 / 88) and most of all one
+    // among idle sequences (256 tokens, 255 idle: 692 / 49).
     const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
     const bool few = L.paged && rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64);
     CUtensorMap mq, mk, mv;
