@@ -407,10 +407,11 @@ CKV_API ckv_status ckv_score_window_static(const ckv_config* cfg, int32_t layer,
  * for the kept rows and the tokens that follow, and the attention of new tokens over it.  A layer's
  * way through them: ckv_prefill_attention -> ckv_compress_layer(s)_lse (with its lse_win) ->
  * ckv_block_tables (the kept lengths) -> ckv_cache_write (k_out, v_out); then per decode step
- * ckv_block_tables -> ckv_cache_write -> ckv_paged_attention.  (The paper's own decoding over the
- * compressed cache is Eq. 3-4; its prefill attention is Eq. 2.)
+ * ckv_block_tables -> ckv_cache_write -> ckv_paged_attention.  Where queries and keys come unrotated,
+ * ckv_cache_append takes the place of ckv_cache_write; ckv_cache_append_q4 and ckv_paged_attention_q4 are the same over a
+ * cache of 4 bits.  (The paper's own decoding over the compressed cache is Eq. 3-4; its prefill attention is Eq. 2.)
  *
- * The workspace of these calls is ckv_attention_workspace_size's (one for all four; ckv_block_tables and
+ * The workspace of these calls is ckv_attention_workspace_size's (one for all of them; ckv_block_tables, the appends and
  * ckv_cache_write touch only its first 1.5 KB, and ask for the whole of it all the same), zeroed once like the others, and again
  * after a status of code 2 (a wait that gave up can leave the count of a unit's parts open); the rules
  * above for workspaces, streams, alignment and errors hold.  Of the config they read the head
@@ -488,6 +489,67 @@ CKV_API ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache*
                                    int64_t tok_stride, int64_t head_stride, const int32_t* slot_map,
                                    void* workspace, size_t workspace_bytes, ckv_stream stream);
 
+/* The rotation of queries and keys by their tokens' positions: of a head's first rotary_dim channels, pair i is turned
+ * by an angle of its own, (a, b) -> (a cos - b sin, b cos + a sin); the other channels pass unchanged.
+ *   cos_sin       device fp32 [num_positions][rotary_dim], 16-byte aligned: a position's rotary_dim / 2 cosines and then
+ *                 as many sines (any scaling of frequencies or amplitudes is the caller's)
+ *   rotary_dim    a multiple of 16, 16..128
+ *   interleaved   0: channel i is paired with i + rotary_dim / 2; 1: channel 2i with 2i + 1
+ * The result is the exact one rounded to fp32 and then to bf16. */
+typedef struct ckv_rotation {
+    const float* cos_sin;
+    int32_t num_positions;
+    int32_t rotary_dim;
+    int32_t interleaved;
+} ckv_rotation;
+
+/* ckv_cache_write with the rotation on the way: k's rows are rotated by their tokens' positions, and so are the queries
+ * of the same tokens, in one launch.  (After a compression a token's index in the cache is not its position, so
+ * positions are an input.)
+ *   q          [num_tokens, H_q, 128] with strides in elements (0 = packed); NULL: no queries
+ *   q_out      [num_tokens, H_q, 128] packed, the rotated queries; may be q itself if that is packed
+ *   k_out      [num_tokens, H_kv, 128] packed, the rotated keys (for the prefill attention or the compression); may be k
+ *              itself if that is packed; may be NULL
+ *   positions  device int32 [num_tokens].  -1: nothing of the token is done (padding); any other outside
+ *              [0, num_positions) likewise, and gives status code 3.
+ *   slot_map   as for ckv_cache_write; of a token without a slot, q_out and k_out are written all the same.
+ * What is written overlaps nothing else that the call is given (host check: CKV_ERR_INVALID_ARG). */
+CKV_API ckv_status ckv_cache_append(const ckv_config* cfg, const ckv_paged_cache* cache, int32_t num_tokens,
+                                    const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* q_out,
+                                    const void* k, const void* v, int64_t tok_stride, int64_t head_stride,
+                                    void* k_out, const ckv_rotation* rotation, const int32_t* positions,
+                                    const int32_t* slot_map, void* workspace, size_t workspace_bytes,
+                                    ckv_stream stream);
+
+/* A paged cache in 4 bits: 72 bytes a row of 128 values.  The tables and slot maps are those of a bf16 cache
+ * (ckv_block_tables).  Page p begins at byte p * page_stride (0 = packed; a multiple of 16) and holds, per KV head,
+ * K's block and then V's, each of page_size * 72 bytes: codes [4 groups][page_size][16 bytes], scales
+ * [page_size][4 groups][2 bytes].
+ *   A group is 32 channels x of a row.  With range = max(x, 0) - min(x, 0): its scale s is the least number of 4
+ *   significant bits, 2^-100 at least, with 15 s >= range; its zero point z = round(-min(x, 0) / s); its codes
+ *   n = clamp(round(x / s) + z, 0, 15), ties to even.  A value is s (n - z), within s / 2 of x, and a bf16 number.
+ *   The 16 bytes of codes are four 32-bit words of 8 channels, channel c of a word in nibble c / 2 + 4 (c % 2) (bits 4 i
+ *   to 4 i + 3); the scale's 16 bits are the bf16 pattern of s, whose low nibble is 0, with z there.
+ *   A group with a NaN or an infinity has a NaN for s: all its values are NaN.  Values are below 1e38 in magnitude.
+ * Rows of a page behind a sequence's end are never used, so pages need no clearing. */
+typedef struct ckv_paged_cache_q4 {
+    void* pages;          /* 16-byte aligned */
+    int64_t page_stride;  /* bytes */
+    int32_t num_pages;
+    int32_t page_size; /* 16, 32, 64 or 128 */
+} ckv_paged_cache_q4;
+
+/* ckv_cache_append into a cache of 4 bits.  Without a rotation (NULL, and then no positions and no queries) the rows
+ * are taken as they are: kept rows of a compressed prompt, whose keys are rotated already.
+ *   k_out, v_out  [num_tokens, H_kv, 128] packed bf16: the values that the cache holds for the rows (what an
+ *                 attention over it will see); may be k and v themselves if those are packed; may be NULL. */
+CKV_API ckv_status ckv_cache_append_q4(const ckv_config* cfg, const ckv_paged_cache_q4* cache, int32_t num_tokens,
+                                       const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* q_out,
+                                       const void* k, const void* v, int64_t tok_stride, int64_t head_stride,
+                                       void* k_out, void* v_out, const ckv_rotation* rotation,
+                                       const int32_t* positions, const int32_t* slot_map, void* workspace,
+                                       size_t workspace_bytes, ckv_stream stream);
+
 /* Attention of new tokens over the paged cache: single tokens, or chunks of them.  Sequence s has n =
  * cu_new[s+1] - cu_new[s] query rows (q rows cu_new[s] - cu_new[0] on) and L = cache_lens[s] cached
  * tokens, the new ones included and written before; its query row i sees keys 0..L - n + i, key j in
@@ -508,6 +570,15 @@ CKV_API ckv_status ckv_paged_attention(const ckv_config* cfg, const ckv_paged_ca
                                        int64_t q_tok_stride, int64_t q_head_stride, void* out,
                                        float* lse, int64_t lse_head_stride, void* workspace,
                                        size_t workspace_bytes, ckv_stream stream);
+
+/* ckv_paged_attention over a cache of 4 bits: the same call, lengths, outputs and status codes.  The values of the cache
+ * enter both products as they are (bf16 numbers). */
+CKV_API ckv_status ckv_paged_attention_q4(const ckv_config* cfg, const ckv_paged_cache_q4* cache,
+                                          int32_t num_seqs, int32_t num_tokens, const int32_t* block_table,
+                                          int32_t max_blocks, const int32_t* cache_lens, const int32_t* cu_new,
+                                          const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* out,
+                                          float* lse, int64_t lse_head_stride, void* workspace,
+                                          size_t workspace_bytes, ckv_stream stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,8 @@ __all__ = [
     "ckv_compress_layers", "ckv_compress_layers_lse", "new_layers_workspace", "ckv_score_windows_lse",
     "PagedCache", "new_paged_cache", "new_attention_workspace", "ckv_attention_workspace_size",
     "ckv_prefill_attention", "ckv_block_tables", "ckv_cache_write", "ckv_paged_attention",
+    "Rotation", "new_rotation", "ckv_cache_append", "PagedCacheQ4", "new_paged_cache_q4", "ckv_cache_append_q4",
+    "ckv_paged_attention_q4",
 ]
 
 POOL_MAX, POOL_AVG = 0, 1
@@ -78,6 +80,16 @@ class _PagedCache(C.Structure):
                 ("num_pages", C.c_int32), ("page_size", C.c_int32)]
 
 
+class _PagedCacheQ4(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_stride", C.c_int64), ("num_pages", C.c_int32),
+                ("page_size", C.c_int32)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("num_positions", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
 def load():
     """Loads libckv.so (built by ``paper_2508_02401_gb300.build``)."""
     global _lib
@@ -90,6 +102,7 @@ def load():
     lib = C.CDLL(path)
     P, I32, I64, SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     cfg, bat, cache = C.POINTER(_Config), C.POINTER(_Batch), C.POINTER(_PagedCache)
+    cache4, rot = C.POINTER(_PagedCacheQ4), C.POINTER(_Rotation)
     sigs = {
         "ckv_abi_version": ([], I32),
         "ckv_status_string": ([C.c_int], C.c_char_p),
@@ -121,6 +134,9 @@ def load():
         "ckv_prefill_attention": ([cfg, bat, P, I64, I64, P, P, I64, I64, P, P, I64, P, I64, P, SZ, P], C.c_int),
         "ckv_block_tables": ([I32, I32, P, P, P, I32, P, P, I32, P, I32, P, P, P, P, SZ, P], C.c_int),
         "ckv_cache_write": ([cfg, cache, I32, P, P, I64, I64, P, P, SZ, P], C.c_int),
+        "ckv_cache_append": ([cfg, cache, I32, P, I64, I64, P, P, P, I64, I64, P, rot, P, P, P, SZ, P], C.c_int),
+        "ckv_cache_append_q4": ([cfg, cache4, I32, P, I64, I64, P, P, P, I64, I64, P, P, rot, P, P, P, SZ, P], C.c_int),
+        "ckv_paged_attention_q4": ([cfg, cache4, I32, I32, P, I32, P, P, P, I64, I64, P, P, I64, P, SZ, P], C.c_int),
         "ckv_paged_attention": ([cfg, cache, I32, I32, P, I32, P, P, P, I64, I64, P, P, I64, P, SZ, P], C.c_int),
     }
     for name, (args, res) in sigs.items():
@@ -544,7 +560,62 @@ def new_paged_cache(cfg, num_pages, page_size, device="cuda"):
     return PagedCache(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
 
 
-def _cache_of(cfg, cache, dev):
+class PagedCacheQ4:
+    """Pages of K and V in 4 bits, uint8 [num_pages, H_kv, 2, page_size * 72] (ckv_paged_cache_q4).  The pages may be
+    strided; a page is packed."""
+
+    def __init__(self, pages, page_size):
+        torch = _torch()
+        if pages.dtype is not torch.uint8 or not pages.is_cuda:
+            raise ValueError(f"pages is {pages.dtype} on {pages.device}, not uint8 on a CUDA device")
+        if pages.dim() != 4 or pages.shape[2] != 2 or pages.shape[3] != page_size * 72:
+            raise ValueError(f"pages is {tuple(pages.shape)}, not [num_pages, H_kv, 2, {page_size} * 72]")
+        row = pages.shape[3]
+        if pages.numel() and pages.stride()[1:] != (2 * row, row, 1):
+            raise ValueError("pages: a page is not packed")
+        if pages.shape[0] > 1 and pages.stride(0) < pages.shape[1] * 2 * row:
+            raise ValueError(f"the pages overlap (page stride {pages.stride(0)})")
+        self.pages, self.page_size = pages, page_size
+        self.num_pages, self.num_kv_heads = pages.shape[:2]
+        self.device_index = pages.get_device()
+        stride = pages.stride(0) if pages.shape[0] > 1 else 0
+        self._c = _PagedCacheQ4(pages.data_ptr(), stride, self.num_pages, page_size)
+        self.ref = C.byref(self._c)
+
+
+def new_paged_cache_q4(cfg, num_pages, page_size, device="cuda"):
+    """A PagedCacheQ4 of uninitialised pages."""
+    shape = (num_pages, cfg.num_kv_heads, 2, page_size * 72)
+    torch = _torch()
+    return PagedCacheQ4(torch.empty(shape, dtype=torch.uint8, device=device), page_size)
+
+
+class Rotation:
+    """The rotation of queries and keys (ckv_rotation): cos_sin float32 [positions, rotary_dim], a position's
+    cosines and then its sines; interleaved: neighbours are paired, not halves."""
+
+    def __init__(self, cos_sin, interleaved=False):
+        torch = _torch()
+        if cos_sin.dtype is not torch.float32 or not cos_sin.is_cuda or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+            raise ValueError(f"cos_sin is {cos_sin.dtype} {tuple(cos_sin.shape)} on {cos_sin.device}, not contiguous "
+                             "float32 [positions, rotary_dim] on a CUDA device")
+        self.cos_sin, self.interleaved = cos_sin, bool(interleaved)
+        self.device_index = cos_sin.get_device()
+        self._c = _Rotation(cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], int(self.interleaved))
+        self.ref = C.byref(self._c)
+
+
+def new_rotation(num_positions, base=10000.0, rotary_dim=128, interleaved=False, device="cuda"):
+    """The Rotation by p * base^(-2 i / rotary_dim) for pair i at position p, its angles taken in 64 bits."""
+    torch = _torch()
+    f = float(base) ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64, device=device) / rotary_dim)
+    angle = torch.arange(num_positions, dtype=torch.float64, device=device)[:, None] * f
+    return Rotation(torch.cat([angle.cos(), angle.sin()], 1).float(), interleaved)
+
+
+def _cache_of(cfg, cache, dev, kind=None):
+    if not isinstance(cache, kind or PagedCache):
+        raise ValueError(f"the cache is a {type(cache).__name__}, not a {(kind or PagedCache).__name__}")
     if cache.num_kv_heads != cfg.num_kv_heads:
         raise ValueError(f"the cache has {cache.num_kv_heads} KV heads, the config {cfg.num_kv_heads}")
     if cache.device_index != dev:
@@ -623,6 +694,63 @@ def ckv_cache_write(cfg, cache, k, v, slot_map, workspace, stream=None, tok_stri
         _check(rc, "ckv_cache_write")
 
 
+def _rotated(rotation, positions, q, q_out, cfg, n, dev, q_tok_stride, q_head_stride):
+    """(rotation, positions, q, q_out) of an append's n tokens."""
+    if rotation is None:
+        if positions is not None or q is not None or q_out is not None:
+            raise ValueError("positions, q and q_out go with a rotation")
+        return None, None, None, None
+    if rotation.device_index != dev:
+        raise ValueError(f"the rotation is on CUDA device {rotation.device_index}, not on the current one, {dev}")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    pos, hq = _packed("positions", positions, _t.int32, dev, n), cfg.num_q_heads
+    if q is None:
+        return rotation.ref, pos, None, None
+    return (rotation.ref, pos, _rows("q", q, dev, n, hq, q_tok_stride, q_head_stride),
+            _packed("q_out", q_out, _t.bfloat16, dev, n * hq * 128))
+
+
+def _out_rows(name, t, cfg, n, dev):
+    return None if t is None else _packed(name, t, _t.bfloat16, dev, n * cfg.num_kv_heads * 128)
+
+
+def ckv_cache_append(cfg, cache, k, v, slot_map, rotation, positions, workspace, q=None, q_out=None, k_out=None,
+                     stream=None, tok_stride=0, head_stride=0, q_tok_stride=0, q_head_stride=0):
+    """k [tokens, H_kv, 128], rotated by the tokens' positions (int32, -1: nothing of the token is done), and v into
+    the cache's slots slot_map [tokens] int32 (-1: not cached); q [tokens, H_q, 128] rotated into q_out, the
+    rotated keys into k_out where given."""
+    dev, stream = _here(stream)
+    n, hkv = slot_map.numel(), cfg.num_kv_heads
+    rot, pos, qp, qo = _rotated(rotation, positions, q, q_out, cfg, n, dev, q_tok_stride, q_head_stride)
+    rc = (_lib or load()).ckv_cache_append(
+        cfg.ref, _cache_of(cfg, cache, dev), n, qp, q_tok_stride, q_head_stride, qo,
+        _rows("k", k, dev, n, hkv, tok_stride, head_stride), _rows("v", v, dev, n, hkv, tok_stride, head_stride),
+        tok_stride, head_stride, _out_rows("k_out", k_out, cfg, n, dev), rot, pos,
+        _packed("slot_map", slot_map, _t.int32, dev, n), _packed("workspace", workspace, _t.uint8, dev, 1),
+        workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_cache_append")
+
+
+def ckv_cache_append_q4(cfg, cache, k, v, slot_map, workspace, rotation=None, positions=None, q=None, q_out=None,
+                        k_out=None, v_out=None, stream=None, tok_stride=0, head_stride=0, q_tok_stride=0,
+                        q_head_stride=0):
+    """ckv_cache_append into a PagedCacheQ4; without a rotation the rows are taken as they are.  k_out and v_out, where
+    given, are the values that the cache holds for the rows."""
+    dev, stream = _here(stream)
+    n, hkv = slot_map.numel(), cfg.num_kv_heads
+    rot, pos, qp, qo = _rotated(rotation, positions, q, q_out, cfg, n, dev, q_tok_stride, q_head_stride)
+    rc = (_lib or load()).ckv_cache_append_q4(
+        cfg.ref, _cache_of(cfg, cache, dev, PagedCacheQ4), n, qp, q_tok_stride, q_head_stride, qo,
+        _rows("k", k, dev, n, hkv, tok_stride, head_stride), _rows("v", v, dev, n, hkv, tok_stride, head_stride),
+        tok_stride, head_stride, _out_rows("k_out", k_out, cfg, n, dev), _out_rows("v_out", v_out, cfg, n, dev), rot, pos,
+        _packed("slot_map", slot_map, _t.int32, dev, n), _packed("workspace", workspace, _t.uint8, dev, 1),
+        workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_cache_append_q4")
+
+
 def ckv_paged_attention(cfg, cache, block_table, cache_lens, cu_new, q, out, workspace, lse=None,
                         lse_head_stride=0, stream=None, q_tok_stride=0, q_head_stride=0):
     """Attention of the new tokens q [tokens, H_q, 128] over the cache: block_table [S, max_blocks],
@@ -637,3 +765,18 @@ def ckv_paged_attention(cfg, cache, block_table, cache_lens, cu_new, q, out, wor
         lse_head_stride, _packed("workspace", workspace, _t.uint8, dev, 1), workspace.numel(), stream)
     if rc:
         _check(rc, "ckv_paged_attention")
+
+
+def ckv_paged_attention_q4(cfg, cache, block_table, cache_lens, cu_new, q, out, workspace, lse=None,
+                           lse_head_stride=0, stream=None, q_tok_stride=0, q_head_stride=0):
+    """ckv_paged_attention over a PagedCacheQ4."""
+    dev, stream = _here(stream)
+    S, hq, T, i32 = cache_lens.numel(), cfg.num_q_heads, q.shape[0], _t.int32
+    rc = (_lib or load()).ckv_paged_attention_q4(
+        cfg.ref, _cache_of(cfg, cache, dev, PagedCacheQ4), S, T, _table("block_table", block_table, S, dev),
+        block_table.shape[1], _packed("cache_lens", cache_lens, i32, dev, S), _packed("cu_new", cu_new, i32, dev, S + 1),
+        _rows("q", q, dev, T, hq, q_tok_stride, q_head_stride), q_tok_stride, q_head_stride,
+        _packed("out", out, _t.bfloat16, dev, T * hq * 128), _lse_of("lse", lse, dev, hq, T, lse_head_stride),
+        lse_head_stride, _packed("workspace", workspace, _t.uint8, dev, 1), workspace.numel(), stream)
+    if rc:
+        _check(rc, "ckv_paged_attention_q4")

@@ -1,0 +1,213 @@
+// New tokens' way into the paged cache: queries and keys are rotated by their tokens' positions, keys and values go into
+// their slots, as bf16 or in 4 bits (kv4.cuh).
+//
+// Rotation of a pair (a, b) by the angle t: (a cos t - b sin t, b cos t + a sin t), with cos and sin from the
+// caller's table.  The result is the exact one rounded to 32 bits and then to bf16, so that a key's codes in 4 bits do
+// not depend on how an fp32 sum happened to be rounded (rotate8).
+//
+// Bound by memory: every row is read once and written once or twice.  A half-warp takes four rows of one token, 16 bytes a
+// lane and row, with the token's angles in registers: loaded once for four rows they cost half of what a row does.
+#include <float.h>
+
+#include "ckv_device.cuh"
+#include "ckv_internal.h"
+#include "kv4.cuh"
+
+namespace ckv {
+namespace {
+
+constexpr int kAppThreads = 256;
+constexpr int kAppToks = kAppThreads / 16;  // tokens of a CTA
+constexpr int kAppQ = 4, kAppKv = 2;        // query heads, KV heads (a row of K and one of V each) of a half-warp
+
+enum { kRotNone = 0, kRotHalves = 1, kRotPairs = 2 };
+
+// The angles of a lane's 8 channels: out_i = x_i c_i + y_i s_i with y_i the other value of the pair.
+struct Angles {
+    float c[8], s[8];
+    int src;      // lane (of 16) that holds the other values (halves)
+    bool active;  // the channels are rotated
+};
+
+template <int ROT>
+__device__ __forceinline__ void load_angles(const AppendLaunch& p, int pos, int c, bool live, Angles& A) {
+    const int half = p.rotary >> 1;
+    A.src = c;
+    A.active = live && c * 8 < p.rotary;
+    const bool upper = ROT == kRotHalves && c * 8 >= half;
+    if (c * 8 < p.rotary && ROT == kRotHalves) A.src = upper ? c - (half >> 3) : c + (half >> 3);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        A.c[i] = 1.f;
+        A.s[i] = 0.f;
+    }
+    if (!A.active) return;
+    const float* row = p.cos_sin + static_cast<size_t>(pos) * p.rotary;
+    if constexpr (ROT == kRotHalves) {
+        const int a = upper ? c * 8 - half : c * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 co = *reinterpret_cast<const float4*>(row + a + i), si = *reinterpret_cast<const float4*>(row + half + a + i);
+            A.c[i] = co.x, A.c[i + 1] = co.y, A.c[i + 2] = co.z, A.c[i + 3] = co.w;
+            A.s[i] = si.x, A.s[i + 1] = si.y, A.s[i + 2] = si.z, A.s[i + 3] = si.w;
+        }
+        if (!upper) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) A.s[i] = -A.s[i];
+        }
+    } else {
+        const float4 co = *reinterpret_cast<const float4*>(row + c * 4), si = *reinterpret_cast<const float4*>(row + half + c * 4);
+        A.c[0] = A.c[1] = co.x, A.c[2] = A.c[3] = co.y, A.c[4] = A.c[5] = co.z, A.c[6] = A.c[7] = co.w;
+        A.s[1] = si.x, A.s[3] = si.y, A.s[5] = si.z, A.s[7] = si.w;
+        A.s[0] = -si.x, A.s[2] = -si.y, A.s[4] = -si.z, A.s[6] = -si.w;
+    }
+}
+
+// A lane's 8 channels of a row, rotated (a whole half-warp).  The fp32 result r is off by 2^-24 (|y s| + |r|) at most;
+// where all of a wider interval rounds to one bf16 number, that is the result, otherwise (1 element in 2000) the sum is
+// taken in 64 bits, where both products are exact.
+template <int ROT>
+__device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
+    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+    uint32_t y[4];
+    if constexpr (ROT == kRotHalves) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], A.src, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __byte_perm(x[i], x[i], 0x1032);
+    }
+    if (!A.active) return x4;
+    uint32_t lo[4], hi[4], differ = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float l[2], h[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float xf = e ? bf16_hi(x[i]) : bf16_lo(x[i]), yf = e ? bf16_hi(y[i]) : bf16_lo(y[i]);
+            const float q = yf * A.s[2 * i + e], r = fmaf(xf, A.c[2 * i + e], q);
+            const float w = fabsf(q) + fabsf(r);
+            l[e] = fmaf(w, -0x1p-23f, r);
+            h[e] = fmaf(w, 0x1p-23f, r);
+        }
+        lo[i] = pack_bf16x2(l[0], l[1]);
+        hi[i] = pack_bf16x2(h[0], h[1]);
+        differ |= lo[i] ^ hi[i];
+    }
+    if (differ) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float r[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const double xd = e ? bf16_hi(x[i]) : bf16_lo(x[i]), yd = e ? bf16_hi(y[i]) : bf16_lo(y[i]);
+                r[e] = static_cast<float>(fma(xd, static_cast<double>(A.c[2 * i + e]), yd * static_cast<double>(A.s[2 * i + e])));
+            }
+            lo[i] = pack_bf16x2(r[0], r[1]);
+        }
+    }
+    return make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+template <bool Q4, int ROT>
+__global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_constant__ AppendLaunch p) {
+    const int c = threadIdx.x & 15;
+    const int nq = p.q ? (p.Hq + kAppQ - 1) / kAppQ : 0, chunks = nq + (p.Hkv + kAppKv - 1) / kAppKv;
+    const int block = blockIdx.x / chunks, ch = blockIdx.x - block * chunks;
+    const int t = block * kAppToks + static_cast<int>(threadIdx.x >> 4);
+    bool live = t < p.T;
+    Angles A;
+    if constexpr (ROT != kRotNone) {
+        const int pos = live ? p.positions[t] : -1;
+        if (pos < 0 || pos >= p.num_positions) {
+            if (pos != -1 && c == 0) record_error(p.status, kDevBadIndex, t);
+            live = false;
+        }
+        load_angles<ROT>(p, pos, c, live, A);
+    }
+    if (ch < nq) {
+        const int h0 = ch * kAppQ;
+        uint4 x[kAppQ];
+#pragma unroll
+        for (int u = 0; u < kAppQ; ++u) {
+            x[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (live && h0 + u < p.Hq)
+                x[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + t * p.q_tok +
+                                                       (h0 + u) * p.q_head + c * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < kAppQ; ++u) {
+            if constexpr (ROT != kRotNone) x[u] = rotate8<ROT>(x[u], A);
+            if (live && h0 + u < p.Hq)
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.q_out) +
+                                          (static_cast<long long>(t) * p.Hq + h0 + u) * kHeadDim + c * 8) = x[u];
+        }
+        return;
+    }
+    const int h0 = (ch - nq) * kAppKv;
+    uint4 k[kAppKv], v[kAppKv];
+#pragma unroll
+    for (int u = 0; u < kAppKv; ++u) {
+        k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && h0 + u < p.Hkv) {
+            const long long src = t * p.tok_stride + (h0 + u) * p.head_stride + c * 8;
+            k[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k) + src);
+            v[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v) + src);
+        }
+    }
+    int slot = live ? p.slots[t] : -1;
+    if (slot < -1 || slot >= p.num_slots) {
+        if (c == 0 && h0 == 0) record_error(p.status, kDevBadIndex, t);
+        slot = -1;
+    }
+    const long long page = slot >> p.shift;
+    const int row = slot & ((1 << p.shift) - 1);
+#pragma unroll
+    for (int u = 0; u < kAppKv; ++u) {
+        if constexpr (ROT != kRotNone) k[u] = rotate8<ROT>(k[u], A);
+        const bool has = live && h0 + u < p.Hkv;
+        const long long to = (static_cast<long long>(t) * p.Hkv + h0 + u) * kHeadDim + c * 8;
+        if constexpr (Q4) {
+            const Kv4Lane kq = kv4_quantise(k[u]), vq = kv4_quantise(v[u]);
+            if (has && slot >= 0) {
+                uint8_t* d = static_cast<uint8_t*>(p.k_pages) + page * p.page_stride +
+                             (static_cast<long long>(h0 + u) << p.shift) * (2 * kKv4RowBytes);
+                kv4_store(d, p.shift, row, c, kq);
+                kv4_store(d + (kKv4RowBytes << p.shift), p.shift, row, c, vq);
+            }
+            if (has && p.k_out) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_out) + to) = kv4_values(kq);
+            if (has && p.v_out) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.v_out) + to) = kv4_values(vq);
+        } else {
+            if (has && slot >= 0) {
+                const long long d = page * p.page_stride + (static_cast<long long>(row) * p.Hkv + h0 + u) * kHeadDim + c * 8;
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_pages) + d) = k[u];
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.v_pages) + d) = v[u];
+            }
+            if (has && p.k_out) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_out) + to) = k[u];
+        }
+    }
+}
+
+template <bool Q4, int ROT>
+cudaError_t launch(const AppendLaunch& L, unsigned grid, cudaStream_t stream) {
+    cache_append_kernel<Q4, ROT><<<grid, kAppThreads, 0, stream>>>(L);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+long long append_blocks(int T, int Hq, int Hkv) {
+    return static_cast<long long>((T - 1) / kAppToks + 1) * ((Hq + kAppQ - 1) / kAppQ + (Hkv + kAppKv - 1) / kAppKv);
+}
+
+cudaError_t launch_cache_append(const AppendLaunch& L, cudaStream_t stream) {
+    const unsigned grid = static_cast<unsigned>(append_blocks(L.T, L.q ? L.Hq : 0, L.Hkv));
+    NvtxRange range("cache_append_kernel");
+    const int rot = !L.cos_sin ? kRotNone : L.interleaved ? kRotPairs : kRotHalves;
+    if (L.q4)
+        return rot == kRotNone ? launch<true, kRotNone>(L, grid, stream)
+               : rot == kRotPairs ? launch<true, kRotPairs>(L, grid, stream) : launch<true, kRotHalves>(L, grid, stream);
+    return rot == kRotPairs ? launch<false, kRotPairs>(L, grid, stream) : launch<false, kRotHalves>(L, grid, stream);
+}
+
+}  // namespace ckv

@@ -1671,6 +1671,20 @@ ckv_status resolve_page_stride(const ckv_paged_cache* c, int Hkv, int64_t* page_
     return CKV_OK;
 }
 
+ckv_status check_cache_q4(const ckv_paged_cache_q4* c, int Hkv, int64_t* page_stride) {
+    if (!c) return fail(CKV_ERR_INVALID_ARG, "cache is NULL");
+    const ckv_paged_cache as = {c->pages, c->pages, 0, c->num_pages, c->page_size};
+    const ckv_status st = check_cache(&as, page_stride);
+    if (st) return st;
+    const int64_t least = static_cast<int64_t>(c->page_size) * Hkv * 144;
+    *page_stride = c->page_stride == 0 ? least : c->page_stride;
+    if (*page_stride < least || *page_stride % 16)
+        return fail(CKV_ERR_INVALID_ARG, "page_stride %lld: a multiple of 16 bytes, at least %lld",
+                    static_cast<long long>(*page_stride), static_cast<long long>(least));
+    if (*page_stride >= (static_cast<int64_t>(1) << 38)) return fail(CKV_ERR_UNSUPPORTED, "page_stride too large");
+    return CKV_OK;
+}
+
 // A bf16 tensor of `rank` dimensions, {128, ...}, 128-byte swizzled like the MMA operands; strides in
 // elements, the innermost being 1.
 ckv_status make_rows_map(CUtensorMap* map, const void* ptr, int rank, const int64_t* dims, const int64_t* strides,
@@ -1741,6 +1755,47 @@ void attn_common(AttnLaunch& L, const ckv_config* cfg, void* workspace, const At
     L.partials = reinterpret_cast<float*>(w8 + l.partials);
 }
 
+// The arguments that the attentions over a paged cache share, into a launch.
+ckv_status paged_attention_args(const ckv_config* cfg, int page_size, int32_t num_seqs, int32_t num_tokens,
+                                const int32_t* block_table, int32_t max_blocks, const int32_t* cache_lens,
+                                const int32_t* cu_new, const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+                                void* out, float* lse, int64_t lse_head_stride, void* workspace,
+                                size_t workspace_bytes, AttnLaunch& L) {
+    ckv_status st;
+    AttnWs l;
+    if (num_seqs < 1) return fail(CKV_ERR_INVALID_ARG, "num_seqs %d < 1", num_seqs);
+    if (num_tokens < 0) return fail(CKV_ERR_INVALID_ARG, "num_tokens %d < 0", num_tokens);
+    if (max_blocks < 1) return fail(CKV_ERR_INVALID_ARG, "max_blocks %d < 1", max_blocks);
+    if (static_cast<int64_t>(max_blocks) * page_size > INT_MAX - 128)
+        return fail(CKV_ERR_UNSUPPORTED, "block-table rows of more than 2^31 - 129 tokens");
+    if (!block_table || !cache_lens || !cu_new)
+        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens and cu_new are required");
+    if (!aligned(block_table, 4) || !aligned(cache_lens, 4) || !aligned(cu_new, 4))
+        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens or cu_new is not 4-byte aligned");
+    if ((st = check_strides("q", cfg->num_q_heads, &q_tok_stride, &q_head_stride)) ||
+        (st = check_kv(q, "q", num_tokens)) || (st = check_kv(out, "out", num_tokens)) ||
+        (st = check_lse_out("lse", lse, num_tokens, &lse_head_stride)) ||
+        (st = check_attn_ws(workspace, workspace_bytes, &l)))
+        return st;
+    memset(&L, 0, sizeof L);
+    attn_common(L, cfg, workspace, l);
+    L.q = q;
+    L.q_tok = q_tok_stride;
+    L.q_head = q_head_stride;
+    L.cu = cu_new;
+    L.lens = cache_lens;
+    L.paged = true;
+    L.page_size = page_size;
+    L.max_blocks = max_blocks;
+    L.table = block_table;
+    L.S = num_seqs;
+    L.T = num_tokens;
+    L.out = out;
+    L.lse = lse;
+    L.lse_stride = lse_head_stride;
+    return CKV_OK;
+}
+
 }  // namespace
 
 ckv_status ckv_attention_workspace_size(const ckv_config* cfg, size_t* bytes) {
@@ -1802,48 +1857,44 @@ ckv_status ckv_paged_attention(const ckv_config* cfg, const ckv_paged_cache* cac
     ckv_status st = check_config(cfg);
     if (st) return st;
     int64_t page_stride = 0;
-    AttnWs l;
     if ((st = check_cache(cache, &page_stride)) || (st = resolve_page_stride(cache, cfg->num_kv_heads, &page_stride)))
         return st;
-    if (num_seqs < 1) return fail(CKV_ERR_INVALID_ARG, "num_seqs %d < 1", num_seqs);
-    if (num_tokens < 0) return fail(CKV_ERR_INVALID_ARG, "num_tokens %d < 0", num_tokens);
-    if (max_blocks < 1) return fail(CKV_ERR_INVALID_ARG, "max_blocks %d < 1", max_blocks);
-    if (static_cast<int64_t>(max_blocks) * cache->page_size > INT_MAX - 128)
-        return fail(CKV_ERR_UNSUPPORTED, "block-table rows of more than 2^31 - 129 tokens");
-    if (!block_table || !cache_lens || !cu_new)
-        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens and cu_new are required");
-    if (!aligned(block_table, 4) || !aligned(cache_lens, 4) || !aligned(cu_new, 4))
-        return fail(CKV_ERR_INVALID_ARG, "block_table, cache_lens or cu_new is not 4-byte aligned");
-    if ((st = check_strides("q", cfg->num_q_heads, &q_tok_stride, &q_head_stride)) ||
-        (st = check_kv(q, "q", num_tokens)) || (st = check_kv(out, "out", num_tokens)) ||
-        (st = check_lse_out("lse", lse, num_tokens, &lse_head_stride)) ||
-        (st = check_attn_ws(workspace, workspace_bytes, &l)))
+    AttnLaunch L;
+    if ((st = paged_attention_args(cfg, cache->page_size, num_seqs, num_tokens, block_table, max_blocks, cache_lens,
+                                   cu_new, q, q_tok_stride, q_head_stride, out, lse, lse_head_stride, workspace,
+                                   workspace_bytes, L)))
         return st;
     if (num_tokens == 0) return CKV_OK;
-    AttnLaunch L;
-    memset(&L, 0, sizeof L);
-    attn_common(L, cfg, workspace, l);
-    L.q = q;
-    L.q_tok = q_tok_stride;
-    L.q_head = q_head_stride;
     L.k = cache->k_pages;
     L.v = cache->v_pages;
     L.tok_stride = static_cast<int64_t>(cfg->num_kv_heads) * kHeadDim;
     L.head_stride = kHeadDim;
-    L.cu = cu_new;
-    L.lens = cache_lens;
-    L.paged = true;
     L.page_stride = page_stride;
-    L.page_size = cache->page_size;
     L.num_pages = cache->num_pages;
-    L.max_blocks = max_blocks;
-    L.table = block_table;
-    L.S = num_seqs;
-    L.T = num_tokens;
-    L.out = out;
-    L.lse = lse;
-    L.lse_stride = lse_head_stride;
     return enqueue_attention(L, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ckv_status ckv_paged_attention_q4(const ckv_config* cfg, const ckv_paged_cache_q4* cache, int32_t num_seqs,
+                                  int32_t num_tokens, const int32_t* block_table, int32_t max_blocks,
+                                  const int32_t* cache_lens, const int32_t* cu_new, const void* q,
+                                  int64_t q_tok_stride, int64_t q_head_stride, void* out, float* lse,
+                                  int64_t lse_head_stride, void* workspace, size_t workspace_bytes,
+                                  ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int64_t page_stride = 0;
+    AttnLaunch L;
+    if ((st = check_cache_q4(cache, cfg->num_kv_heads, &page_stride)) ||
+        (st = paged_attention_args(cfg, cache->page_size, num_seqs, num_tokens, block_table, max_blocks, cache_lens,
+                                   cu_new, q, q_tok_stride, q_head_stride, out, lse, lse_head_stride, workspace,
+                                   workspace_bytes, L)))
+        return st;
+    if (num_tokens == 0) return CKV_OK;
+    L.k = cache->pages;
+    L.page_stride = page_stride;
+    L.num_pages = cache->num_pages;
+    const cudaError_t e = launch_attention_q4(L, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 
 ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* cache_lens,
@@ -1955,6 +2006,140 @@ ckv_status ckv_cache_write(const ckv_config* cfg, const ckv_paged_cache* cache, 
     L.status = static_cast<int*>(workspace);
     const cudaError_t e = launch_cache_write(L, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the cache-write kernel");
+}
+
+namespace {
+
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+    const uintptr_t u = reinterpret_cast<uintptr_t>(a.p), v = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && u < v + static_cast<uintptr_t>(b.bytes) && v < u + static_cast<uintptr_t>(a.bytes);
+}
+Span rows_span(const void* p, int T, int heads, int64_t tok, int64_t head) {
+    return {p, ((T - 1) * tok + (heads - 1) * head + kHeadDim) * 2};
+}
+
+// The appends: `L` has the cache's fields and q4.
+ckv_status enqueue_append(const ckv_config* cfg, AppendLaunch& L, int page_size, int num_pages, int32_t num_tokens,
+                          const void* q, int64_t q_tok, int64_t q_head, void* q_out, const void* k, const void* v,
+                          int64_t tok, int64_t head, void* k_out, void* v_out, const ckv_rotation* rot,
+                          const int32_t* positions, const int32_t* slot_map, void* workspace, size_t workspace_bytes,
+                          cudaStream_t stream) {
+    if (num_tokens < 0) return fail(CKV_ERR_INVALID_ARG, "num_tokens %d < 0", num_tokens);
+    const int T = num_tokens, Hq = cfg->num_q_heads, Hkv = cfg->num_kv_heads;
+    ckv_status st;
+    AttnWs l;
+    if ((st = check_strides("k/v", Hkv, &tok, &head)) || (st = check_strides("q", Hq, &q_tok, &q_head)) ||
+        (st = check_kv(k, "k", T)) || (st = check_kv(v, "v", T)) || (st = check_attn_ws(workspace, workspace_bytes, &l)))
+        return st;
+    if (!rot && (q || positions))
+        return fail(CKV_ERR_INVALID_ARG, "without a rotation there are no queries and no positions");
+    if (rot) {
+        if (!rot->cos_sin || !aligned(rot->cos_sin, 16))
+            return fail(CKV_ERR_INVALID_ARG, "cos_sin is required, 16-byte aligned");
+        if (rot->num_positions < 1) return fail(CKV_ERR_INVALID_ARG, "num_positions %d < 1", rot->num_positions);
+        if (rot->rotary_dim < 16 || rot->rotary_dim > kHeadDim || rot->rotary_dim % 16)
+            return fail(CKV_ERR_INVALID_ARG, "rotary_dim %d: a multiple of 16, 16 to 128", rot->rotary_dim);
+        if (rot->interleaved != 0 && rot->interleaved != 1)
+            return fail(CKV_ERR_INVALID_ARG, "interleaved %d: 0 or 1", rot->interleaved);
+    }
+    if (!q != !q_out) return fail(CKV_ERR_INVALID_ARG, "q and q_out go together");
+    if (T == 0) return CKV_OK;
+    if (!slot_map || !aligned(slot_map, 4)) return fail(CKV_ERR_INVALID_ARG, "slot_map is required, 4-byte aligned");
+    if (rot && (!positions || !aligned(positions, 4)))
+        return fail(CKV_ERR_INVALID_ARG, "positions are required, 4-byte aligned");
+    if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(v_out, 16))
+        return fail(CKV_ERR_INVALID_ARG, "q, q_out, k_out or v_out is not 16-byte aligned");
+    if (append_blocks(T, Hq, Hkv) > INT_MAX) return fail(CKV_ERR_UNSUPPORTED, "too many tokens for one call");
+    // A row is read whole before it is written, by the threads that write it: q_out may be q, k_out k and v_out v,
+    // row for row.  Nothing else of what is written may lie over anything.
+    const bool q_packed = q_tok == static_cast<int64_t>(Hq) * kHeadDim && q_head == kHeadDim,
+               kv_packed = tok == static_cast<int64_t>(Hkv) * kHeadDim && head == kHeadDim;
+    const Span in[] = {rows_span(q, T, Hq, q_tok, q_head), rows_span(k, T, Hkv, tok, head), rows_span(v, T, Hkv, tok, head),
+                       {slot_map, 4ll * T}, {positions, 4ll * T},
+                       {rot ? rot->cos_sin : nullptr, rot ? 4ll * rot->num_positions * rot->rotary_dim : 0}};
+    const int64_t pages = (num_pages - 1) * L.page_stride * (L.q4 ? 1 : 2) + static_cast<int64_t>(page_size) * Hkv * (L.q4 ? 144 : 256);
+    const Span out[] = {rows_span(q_out, T, Hq, static_cast<int64_t>(Hq) * kHeadDim, kHeadDim),
+                        rows_span(k_out, T, Hkv, static_cast<int64_t>(Hkv) * kHeadDim, kHeadDim),
+                        rows_span(v_out, T, Hkv, static_cast<int64_t>(Hkv) * kHeadDim, kHeadDim),
+                        {L.k_pages, pages}, {L.v_pages, pages}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < 6; ++j)
+            if (overlap(out[i], in[j]) && !(i == j && i < 3 && out[i].p == in[j].p && (i == 0 ? q_packed : kv_packed)))
+                return fail(CKV_ERR_INVALID_ARG, "what the call writes lies over one of its inputs");
+        for (int j = i + 1; j < 5; ++j)  // (K's and V's pages may alternate in one buffer)
+            if (i < 3 && overlap(out[i], out[j])) return fail(CKV_ERR_INVALID_ARG, "two of the outputs overlap");
+    }
+    L.q = q;
+    L.q_tok = q_tok;
+    L.q_head = q_head;
+    L.q_out = q_out;
+    L.k = k;
+    L.v = v;
+    L.tok_stride = tok;
+    L.head_stride = head;
+    L.k_out = k_out;
+    L.v_out = v_out;
+    L.slots = slot_map;
+    L.positions = positions;
+    L.cos_sin = rot ? rot->cos_sin : nullptr;
+    L.num_positions = rot ? rot->num_positions : 0;
+    L.rotary = rot ? rot->rotary_dim : 0;
+    L.interleaved = rot && rot->interleaved;
+    L.T = T;
+    L.Hq = Hq;
+    L.Hkv = Hkv;
+    L.shift = 0;
+    while ((1 << L.shift) < page_size) ++L.shift;
+    L.num_slots = num_pages * page_size;
+    L.status = static_cast<int*>(workspace);
+    const cudaError_t e = launch_cache_append(L, stream);
+    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the cache-append kernel");
+}
+
+}  // namespace
+
+ckv_status ckv_cache_append(const ckv_config* cfg, const ckv_paged_cache* cache, int32_t num_tokens, const void* q,
+                            int64_t q_tok_stride, int64_t q_head_stride, void* q_out, const void* k, const void* v,
+                            int64_t tok_stride, int64_t head_stride, void* k_out, const ckv_rotation* rotation,
+                            const int32_t* positions, const int32_t* slot_map, void* workspace,
+                            size_t workspace_bytes, ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int64_t page_stride = 0;
+    if ((st = check_cache(cache, &page_stride)) || (st = resolve_page_stride(cache, cfg->num_kv_heads, &page_stride)))
+        return st;
+    if (!rotation) return fail(CKV_ERR_INVALID_ARG, "rotation is NULL (ckv_cache_write takes rows as they are)");
+    AppendLaunch L;
+    memset(&L, 0, sizeof L);
+    L.k_pages = cache->k_pages;
+    L.v_pages = cache->v_pages;
+    L.page_stride = page_stride;
+    return enqueue_append(cfg, L, cache->page_size, cache->num_pages, num_tokens, q, q_tok_stride, q_head_stride, q_out,
+                          k, v, tok_stride, head_stride, k_out, nullptr, rotation, positions, slot_map, workspace,
+                          workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+ckv_status ckv_cache_append_q4(const ckv_config* cfg, const ckv_paged_cache_q4* cache, int32_t num_tokens,
+                               const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* q_out, const void* k,
+                               const void* v, int64_t tok_stride, int64_t head_stride, void* k_out, void* v_out,
+                               const ckv_rotation* rotation, const int32_t* positions, const int32_t* slot_map,
+                               void* workspace, size_t workspace_bytes, ckv_stream stream) {
+    ckv_status st = check_config(cfg);
+    if (st) return st;
+    int64_t page_stride = 0;
+    if ((st = check_cache_q4(cache, cfg->num_kv_heads, &page_stride))) return st;
+    AppendLaunch L;
+    memset(&L, 0, sizeof L);
+    L.q4 = true;
+    L.k_pages = cache->pages;
+    L.page_stride = page_stride;
+    return enqueue_append(cfg, L, cache->page_size, cache->num_pages, num_tokens, q, q_tok_stride, q_head_stride, q_out,
+                          k, v, tok_stride, head_stride, k_out, v_out, rotation, positions, slot_map, workspace,
+                          workspace_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 // The items per unit of a multi-layer launch, for the tests (host only; not part of the ABI): sequence s

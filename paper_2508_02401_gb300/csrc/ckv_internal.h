@@ -274,6 +274,32 @@ struct CacheWriteLaunch {
     int* status;
 };
 cudaError_t launch_cache_write(const CacheWriteLaunch& L, cudaStream_t stream);
+// Rotated rows into the cache (cache_append.cu).
+struct AppendLaunch {
+    const void* q;                  // [T, H_q, 128], or null
+    int64_t q_tok, q_head;
+    void* q_out;                    // [T, H_q, 128] packed
+    const void* k;
+    const void* v;
+    int64_t tok_stride, head_stride;
+    void* k_out;                    // [T, H_kv, 128] packed, or null
+    void* v_out;
+    const int32_t* slots;           // [T], -1: not cached
+    const int32_t* positions;       // [T], -1: nothing of the token is done
+    const float* cos_sin;           // [num_positions][rotary]: cosines, then sines; null: no rotation
+    int num_positions, rotary;
+    bool interleaved, q4;
+    void* k_pages;                  // q4: the pages
+    void* v_pages;
+    int64_t page_stride;            // elements; q4: bytes
+    int T, Hq, Hkv, shift, num_slots;
+    int* status;
+};
+long long append_blocks(int T, int Hq, int Hkv);  // CTAs (Hq: 0 without queries)
+cudaError_t launch_cache_append(const AppendLaunch& L, cudaStream_t stream);
+
+// Attention over a cache of 4 bits: AttnLaunch::k are its pages, page_stride is in bytes.
+cudaError_t launch_attention_q4(const AttnLaunch& L, cudaStream_t stream);
 
 int device_sm_count();
 
