@@ -98,6 +98,15 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+        "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -200,14 +209,15 @@ struct RunStart {
     Seq q;
     int s;
 };
-constexpr int kScanBytes = 14 * 8 + static_cast<int>(sizeof(RunStart)) + 14 * 4;
+constexpr int kScanWarps = 16;
+constexpr int kScanBytes = kScanWarps * 8 + static_cast<int>(sizeof(RunStart)) + kScanWarps * 4;
 
 // Whole block; false (for all of it): nothing to do.  `scan`: kScanBytes of shared memory, the RunStart in it
 // to be read after the next barrier.
-__device__ __forceinline__ RunStart* run_start(long long* scan) { return reinterpret_cast<RunStart*>(scan + 14); }
+__device__ __forceinline__ RunStart* run_start(long long* scan) { return reinterpret_cast<RunStart*>(scan + kScanWarps); }
 template <int THREADS>
 __device__ __forceinline__ bool find_run(const AttnParams& p, int tq, int heads, long long* scan, Run& r) {
-    static_assert(THREADS / 32 <= 14, "scan");
+    static_assert(THREADS / 32 <= kScanWarps, "scan");
     const AttnLaunch& a = p.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cu0 = a.cu[0];
@@ -416,6 +426,17 @@ __device__ __forceinline__ void write_lse(const AttnLaunch& a, const Item& I, in
 }
 
 // ---------------------------------------------------------------------------- K and V tiles
+// Block b's page; num_pages for one that is out of range (reported) as for one beyond the last: it is not loaded, or the load
+// fills with zeros.
+__device__ __forceinline__ int table_page(const AttnLaunch& a, int seq, const int* row, int b) {
+    int pg = row[b];
+    if (pg < 0 || pg >= a.num_pages) {
+        record_error(a.status, kDevBadIndex, seq);
+        pg = a.num_pages;
+    }
+    return pg;
+}
+
 // One warp loads an item's tiles into the ring: K0 V0 K1 V1 ...
 template <bool PAGED, int RING>
 struct TileLoader {
@@ -462,15 +483,7 @@ struct TileLoader {
         const int* row = PAGED ? a.table + static_cast<size_t>(I.seq) * a.max_blocks : nullptr;
         auto window = [&](int u) {
             const int b = ((I.t0 + u) << ppt_shift) + static_cast<int>(threadIdx.x & 31);
-            int pg = a.num_pages;  // beyond the last page: the load fills with zeros
-            if (PAGED && b < blocks && u < I.n_tiles) {
-                pg = row[b];
-                if (pg < 0 || pg >= a.num_pages) {
-                    record_error(a.status, kDevBadIndex, I.seq);
-                    pg = a.num_pages;
-                }
-            }
-            return pg;
+            return PAGED && b < blocks && u < I.n_tiles ? table_page(a, I.seq, row, b) : a.num_pages;
         };
         const int per = 1 << win_shift;
         int now = PAGED ? window(0) : 0, ahead = PAGED ? window(per) : 0;

@@ -1893,7 +1893,10 @@ ckv_status ckv_paged_attention_q4(const ckv_config* cfg, const ckv_paged_cache_q
     L.k = cache->pages;
     L.page_stride = page_stride;
     L.num_pages = cache->num_pages;
-    const cudaError_t e = launch_attention_q4(L, reinterpret_cast<cudaStream_t>(stream));
+    const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
+    const bool few = rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64);
+    const cudaError_t e = few ? launch_attention_few_q4(L, static_cast<int>(rows), reinterpret_cast<cudaStream_t>(stream))
+                              : launch_attention_q4(L, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 

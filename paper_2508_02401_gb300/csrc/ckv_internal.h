@@ -300,6 +300,8 @@ cudaError_t launch_cache_append(const AppendLaunch& L, cudaStream_t stream);
 
 // Attention over a cache of 4 bits: AttnLaunch::k are its pages, page_stride is in bytes.
 cudaError_t launch_attention_q4(const AttnLaunch& L, cudaStream_t stream);
+// Units of 4, 8 or 16 rows, as launch_attention_few (attention_few_q4.cu).
+cudaError_t launch_attention_few_q4(const AttnLaunch& L, int rows, cudaStream_t stream);
 
 int device_sm_count();
 

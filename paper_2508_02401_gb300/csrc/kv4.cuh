@@ -115,6 +115,34 @@ __device__ __forceinline__ Kv4Lane kv4_quantise(const uint4& x4) {
     return q;
 }
 
+// A row's 64 bytes of codes and its four scale words, from a block of a page of 1 << shift tokens in shared memory.
+struct Kv4Row {
+    uint4 codes[4];
+    uint2 scales;
+};
+__device__ __forceinline__ Kv4Row kv4_row(const uint8_t* block, int shift, int row) {
+    Kv4Row r;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) r.codes[g] = *reinterpret_cast<const uint4*>(block + (((g << shift) + row) << 4));
+    r.scales = *reinterpret_cast<const uint2*>(block + (64 << shift) + row * 8);
+    return r;
+}
+// Group g's 32 values as 16 bf16 pairs.
+__device__ __forceinline__ void kv4_group(const Kv4Row& r, int g, uint32_t (&v)[16]) {
+    uint32_t s2, z2;
+    const uint32_t pair = g < 2 ? r.scales.x : r.scales.y;
+    kv4_scale(g & 1 ? pair >> 16 : pair & 0xffffu, s2, z2);
+    const uint32_t w[4] = {r.codes[g].x, r.codes[g].y, r.codes[g].z, r.codes[g].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 x = kv4_word(w[i], s2, z2);
+        v[4 * i] = x.x;
+        v[4 * i + 1] = x.y;
+        v[4 * i + 2] = x.z;
+        v[4 * i + 3] = x.w;
+    }
+}
+
 // The lane's share into `row` of a page's K or V block of one head.
 __device__ __forceinline__ void kv4_store(uint8_t* block, int shift, int row, int c, const Kv4Lane& q) {
     *reinterpret_cast<uint32_t*>(block + ((((c >> 2) << shift) + row) << 4) + ((c & 3) << 2)) = q.word;

@@ -1,0 +1,87 @@
+// Tiles of 128 cached rows in 4 bits, from the pages into a ring of shared memory.
+#pragma once
+
+#include "attention_common.cuh"
+#include "kv4.cuh"
+
+namespace ckv {
+namespace {
+
+constexpr int kPackedTile = 2 * kKv4RowBytes * kTileKeys;  // K and V of 128 tokens of a head: 18 KB
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// One warp loads an item's tiles into the ring, a page a lane: a head's K and V of a page lie together, so a page is
+// one copy (a multiple of 2304 bytes at such an offset: the 16-byte rule of copies holds for any page size).
+template <int RING>
+struct PackedLoader {
+    const AttnParams& p;
+    uint8_t* ring;
+    uint64_t* full;
+    uint64_t* freed;
+    volatile int* abort;
+    long long lim;
+    uint32_t slot = 0, phase = 1, use = 0;
+
+    __device__ bool load(const Item& I, int page, int first) {
+        if (!warp_wait(&freed[slot], phase, abort, lim)) return false;
+        const AttnLaunch& a = p.a;
+        const int lane = threadIdx.x & 31;
+        const uint32_t bytes = (2 * kKv4RowBytes) << p.page_shift;
+        const bool mine = lane >= first && lane < first + (kTileKeys >> p.page_shift) && page < a.num_pages;
+        const uint32_t pages = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) mbar_arrive_expect_tx(&full[slot], pages * bytes);
+        __syncwarp();
+        if (mine)
+            bulk_load(ring + slot * kPackedTile + (lane - first) * bytes,
+                      static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * bytes, bytes, &full[slot]);
+        __syncwarp();
+        ++use;
+        if (++slot == RING) {
+            slot = 0;
+            phase ^= 1;
+        }
+        return true;
+    }
+
+    __device__ bool item(const Item& I) {
+        // Page indices: lane l holds block l of a window of 32 blocks, the next window's at hand.
+        const AttnLaunch& a = p.a;
+        const int ppt_shift = 7 - p.page_shift, win_shift = 5 - ppt_shift;  // pages a tile, tiles a window
+        const int blocks = (I.len + a.page_size - 1) >> p.page_shift;
+        const int* row = a.table + static_cast<size_t>(I.seq) * a.max_blocks;
+        auto window = [&](int u) {
+            const int b = ((I.t0 + u) << ppt_shift) + static_cast<int>(threadIdx.x & 31);
+            return b < blocks && u < I.n_tiles ? table_page(a, I.seq, row, b) : a.num_pages;
+        };
+        const int per = 1 << win_shift;
+        int now = window(0), ahead = window(per);
+        for (int u = 0; u < I.n_tiles; ++u) {
+            if (u > 0 && (u & (per - 1)) == 0) {
+                now = ahead;
+                ahead = window(u + per);
+            }
+            if (!load(I, now, (u & (per - 1)) << ppt_shift)) return false;
+        }
+        return true;
+    }
+
+    // Lets every issued copy land, before the block may exit: others' waits for them may have given up.
+    __device__ void drain() {
+        volatile int never = 0;
+        for (uint32_t k = use > RING ? use - RING : 0; k < use; ++k) mbar_wait(&full[k % RING], (k / RING) & 1, &never);
+    }
+};
+
+// The block of a tile's row (a key of the tile), and the row in its page.
+__device__ __forceinline__ Kv4Row packed_row(const uint8_t* tile, int shift, int key, bool v) {
+    const uint8_t* block = tile + (static_cast<uint32_t>(key >> shift) * 2 + (v ? 1 : 0)) * (kKv4RowBytes << shift);
+    return kv4_row(block, shift, key & ((1 << shift) - 1));
+}
+
+}  // namespace
+}  // namespace ckv
