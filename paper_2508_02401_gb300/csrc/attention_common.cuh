@@ -425,6 +425,52 @@ __device__ __forceinline__ void write_lse(const AttnLaunch& a, const Item& I, in
     }
 }
 
+// Row x of a unit (token tx, head hx) out of its parts, by a warp: a lane holds a part's weight and, of the row, four dims.
+template <int ROWS>
+__device__ __forceinline__ void join_row(const AttnLaunch& a, const Item& I, int x, int tx, int hx) {
+    const int lane = threadIdx.x & 31;
+    float M = -INFINITY, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < I.n_parts; k0 += 32) {
+        const int n = min(32, I.n_parts - k0);
+        float pm = -INFINITY, pl = 0.f;
+        if (lane < n) {
+            const float* src = partial_of<ROWS>(a, I.cta0 + k0 + lane, k0 + lane == 0);
+            pm = __ldcg(src + ROWS * 128 + x);
+            pl = __ldcg(src + ROWS * 129 + x);
+        }
+        const float Mn = fmaxf(M, redux_max(pm));
+        const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
+        const float w = pm == -INFINITY ? 0.f : ex2_approx(pm - Mn);  // (0: no key seen)
+        M = Mn;
+        L = L * f0 + warp_sum(pl * w);
+        acc = make_float4(acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0);
+#pragma unroll 1
+        for (int k = 0; k < n; k += 8) {
+            float4 o[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+                o[y] = k + y < n ? __ldcg(reinterpret_cast<const float4*>(
+                                       partial_of<ROWS>(a, I.cta0 + k0 + k + y, k0 + k + y == 0) + x * 128) + lane)
+                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float wy = __shfl_sync(0xffffffffu, w, (k + y) & 31);
+                if (k + y >= n) continue;
+                acc.x += o[y].x * wy;
+                acc.y += o[y].y * wy;
+                acc.z += o[y].z * wy;
+                acc.w += o[y].w * wy;
+            }
+        }
+    }
+    const float inv = 1.f / L;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
+                         (static_cast<long long>(I.q_row + tx) * a.Hq + I.head0 + hx) * kHeadDim + lane * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (lane == 0) write_lse<false>(a, I, tx, hx, M, L);
+}
+
 // ---------------------------------------------------------------------------- K and V tiles
 // Block b's page; num_pages for one that is out of range (reported) as for one beyond the last: it is not loaded, or the load
 // fills with zeros.

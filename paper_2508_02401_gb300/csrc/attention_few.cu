@@ -8,7 +8,7 @@
 // Bound by the loads of K and V: 64 KB a key tile, 1.5 us of an SM's share of the bandwidth (8 caches of 131072
 // tokens, 4.3 GB: 620 us, 6.9 TB/s).  Two CTAs run on an SM, so that one's start and end of a unit lie beside the
 // other's loads; what they do not hide shows on short caches (256 of 300 tokens, 319 MB: 61 us).
-#include "attention_few.cuh"
+#include "attention_common.cuh"
 
 namespace ckv {
 namespace {
@@ -16,16 +16,20 @@ namespace {
 constexpr int kThreadsF = 256;
 constexpr int kMmaWarpF = 4, kLoadWarpF = 5, kQWarpF = 6;  // warps 0-3: softmax; 7: idle
 
+constexpr int kN = 16;        // (token, head) columns of the MMAs
 constexpr int kCtasF = 2;     // on an SM
 constexpr int kRingF = 3;     // K and V tiles of 32 KB
+constexpr int kQBytesF = kN * 256, kPBytesF = kN * 256;
 constexpr int kTmemF = 64;    // columns: two S, one O (48)
+// P as the second MMA's B: rows of 32 bytes a key, swizzled over as many; 8-key groups of 256 bytes.
+constexpr uint32_t kPGroup = 256, kPHi = (kPGroup >> 4) | (1u << 14) | (6u << 29);
 
 struct FewSmem {
     static constexpr int kQ = kRingF * kTileBytes;
     static constexpr int kP = kQ + 2 * kQBytesF;
-    static constexpr int kRed = kP + kPBytesF;
-    static constexpr int kRef = kRed + kRedBytesF;
-    static constexpr int kItems = kRef + kRefBytesF;
+    static constexpr int kRed = kP + kPBytesF;   // float [4][kN]
+    static constexpr int kRef = kRed + 16 * kN;  // float [kN]: the rows' references, times c
+    static constexpr int kItems = kRef + 4 * kN;
     static constexpr int kBars = kItems + kAttnItemRing * static_cast<int>(sizeof(Item));
     static constexpr int kFull = 0, kFree = kFull + kRingF, kQFull = kFree + kRingF, kQFree = kQFull + 2,
                          kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 1, kItemFull = kPvDone + 1,
@@ -37,10 +41,56 @@ struct FewSmem {
 static_assert(FewSmem::kBytes <= 115712, "shared memory of two CTAs");
 static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * kN * 130 <= kAttnPartialFloats, "workspace");
 
+// Barriers of the softmax warps.  None leaves without the others: they agree on every item, and no wait for a
+// tile makes one leave.
+__device__ __forceinline__ void group_bar() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool group_or(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(x ? 1u : 0u)
+        : "memory");
+    return r != 0;
+}
+
+// COLS (4, 8 or 16) columns of a thread's lane; complete on return.
+template <int COLS>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float* v) {
+    if constexpr (COLS == 4) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(taddr) : "memory");
+    } else if constexpr (COLS == 8) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                     : "r"(taddr) : "memory");
+    } else {
+        tmem_ld16_nowait(taddr, reinterpret_cast<float(&)[16]>(*v));
+    }
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) asm volatile("" : "+f"(v[i]));
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const float* v) {
+    if constexpr (COLS == 4) {
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                     "f"(v[3]) : "memory");
+    } else if constexpr (COLS == 8) {
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "f"(v[0]), "f"(v[1]),
+                     "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+    } else {
+        tmem_st16(taddr, reinterpret_cast<const float(&)[16]>(*v));
+    }
+}
+
 // COLS of the 16 columns hold rows (4, 8 or 16): the others' numerators stay zero.
 template <int COLS>
 __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const __grid_constant__ AttnParams p) {
     using C = FewSmem;
+    constexpr uint32_t kIdescS = idesc_bf16_f32(128, kN);
+    constexpr uint32_t kIdescO = idesc_bf16_f32(128, kN) | (1u << 15) | (1u << 16);  // A and B with M, N contiguous
     extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t* ring = sm;
     uint8_t* qbuf = sm + C::kQ;
@@ -115,7 +165,6 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
     }
     const uint32_t tm_s = *tmem_slot, tm_o = tm_s + 2 * kN;  // S of even and odd tiles, O
     const long long lim = p.wait_cycles;
-    const FewRoles R{qbuf, pbuf, red, ref, items, item_full, item_free, q_full, q_free, s_full, p_full, pv_done, abort, verdict, tm_s, tm_o};
 
     if (warp == kLoadWarpF) {
         // ---------------------------------------------------------------- items, K and V tiles
@@ -142,7 +191,37 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
         tiles.drain();
         __syncwarp();
     } else if (warp == kQWarpF) {
-        few_query_role(p, R, lim);
+        // ---------------------------------------------------------------- query rows
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing, qs = it & 1;
+            if (!(ok = warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim))) break;
+            const Item I = items[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&item_free[slot]);
+            if (I.part == kEndItem) break;
+            if (!(ok = warp_wait(&q_free[qs], ((it >> 1) & 1) ^ 1, abort, lim))) break;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
+            uint8_t* dst = qbuf + qs * kQBytesF;
+            const int chunks = p.tp * p.hp * 16;
+#pragma unroll 4
+            for (int x = lane; x < chunks; x += 32) {
+                const int r = x >> 4, ch = x & 15;
+                const int t = r / p.hp, h = r - t * p.hp;
+                if (t >= I.ntok) continue;
+                const uint4 val = *reinterpret_cast<const uint4*>(
+                    src + (I.q_row + t) * a.q_tok + (I.head0 + h) * a.q_head + ch * 8);
+                *reinterpret_cast<uint4*>(dst + (ch >> 3) * (kN * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = val;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[qs]);
+            __syncwarp();
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 53);
+        }
     } else if (warp == kMmaWarpF) {
         // ---------------------------------------------------------------- MMA issuer
         // The logits of a tile before the product of the one before it: S has two buffers, and the numerators of a
@@ -181,7 +260,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
                     umma_ss<kDescHi>(d_tmem, k_lo + (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2,
-                                     q_lo + (kk >> 2) * (kN * 128 >> 4) + (kk & 3) * 2, kIdescFewS, kk > 0 ? 1u : 0u);
+                                     q_lo + (kk >> 2) * (kN * 128 >> 4) + (kk & 3) * 2, kIdescS, kk > 0 ? 1u : 0u);
                 umma_commit(&s_full[sn & 1]);
                 if (live) umma_commit(&freed[ks]);
                 if (last) umma_commit(&q_free[qs]);
@@ -211,7 +290,7 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
-                        umma_ss<kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * kPGroup >> 4), kIdescFewO,
+                        umma_ss<kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * kPGroup >> 4), kIdescO,
                                          kk > 0 ? 1u : accumulate);
                     umma_commit(pv_done);
                     if (live) umma_commit(&freed[vs]);
@@ -234,7 +313,176 @@ __global__ void __launch_bounds__(kThreadsF, kCtasF) attention_few_kernel(const 
         mbar_wait(done, 0, &never);
         __syncwarp();
     } else if (warp < 4) {
-        few_softmax_role<COLS>(p, R, lim);
+        // ---------------------------------------------------------------- softmax, a key a thread
+        const int key = threadIdx.x;
+        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+        const float c = p.c;
+        uint32_t sn = 0;
+        bool ok = true;
+        float l[COLS];  // this thread's keys' sums
+        // The product of the tile before the current one is in O, and its numerators have been read.
+        auto wait_pv = [&](uint32_t tile) {
+            if (tile == 0) return;
+            tile_wait(pv_done, (tile - 1) & 1, abort, lim, a.status);
+            __syncwarp();
+            tc_fence_after_sync();
+        };
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing;
+            ok = !group_or(!warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim));
+            if (!ok) break;
+            const Item I = items[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&item_free[slot]);
+            if (I.part == kEndItem) break;
+#pragma unroll
+            for (int x = 0; x < COLS; ++x) l[x] = 0.f;
+            if (key < COLS) ref[key] = -INFINITY;
+            group_bar();
+            const int rows = I.ntok * p.hp;
+            // The first key that some row does not see.
+            const int first_end = I.pos0 + 1;
+            for (int i = 0; i < I.n_tiles; ++i, ++sn) {
+                const int k0 = (I.t0 + i) * kTileKeys;
+                tile_wait(&s_full[sn & 1], (sn >> 1) & 1, abort, lim, a.status);
+                __syncwarp();
+                tc_fence_after_sync();
+                float s[COLS];
+                tmem_load<COLS>(tm_s + (sn & 1) * kN + lane_base, s);
+                tc_fence_before_sync();
+                if (k0 + kTileKeys > first_end) {
+                    int ends = first_end - (k0 + key), h = 0;  // positive: the row of column x sees the key
+#pragma unroll
+                    for (int x = 0; x < COLS; ++x) {
+                        s[x] = ends > 0 ? s[x] : -INFINITY;
+                        if (++h == p.hp) {
+                            h = 0;
+                            ++ends;
+                        }
+                    }
+                }
+                float over = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) {
+                    s[x] *= c;
+                    over = fmaxf(over, x < rows ? s[x] - ref[x] : -INFINITY);
+                }
+                if (group_or(over > kAttnTau)) {
+                    wait_pv(sn);
+                    // Move the references that a key passes by more than 2^8 (or that have none yet).
+#pragma unroll
+                    for (int x = 0; x < COLS; ++x) {
+                        const float w = redux_max(s[x]);
+                        if (lane == 0) red[warp * COLS + x] = w;
+                    }
+                    group_bar();
+                    float o[COLS];
+                    if (i > 0) tmem_load<COLS>(tm_o + lane_base, o);
+#pragma unroll
+                    for (int x = 0; x < COLS; ++x) {
+                        const float mx = fmaxf(fmaxf(red[x], red[COLS + x]), fmaxf(red[2 * COLS + x], red[3 * COLS + x]));
+                        const float f = mx - ref[x] > kAttnTau ? ex2_approx(ref[x] - mx) : 1.f;  // (no: -inf - -inf)
+                        l[x] *= f;
+                        o[x] *= f;
+                    }
+                    if (i > 0) tmem_store<COLS>(tm_o + lane_base, o);
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    group_bar();  // ref is read
+                    if (key < COLS) {
+                        const float mx = fmaxf(fmaxf(red[key], red[COLS + key]), fmaxf(red[2 * COLS + key], red[3 * COLS + key]));
+                        if (mx - ref[key] > kAttnTau) ref[key] = mx;
+                    }
+                    group_bar();
+                }
+                uint32_t pk[COLS / 2];
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) {
+                    s[x] = ex2_approx(s[x] - fmaxf(ref[x], -3e38f));  // (-inf: a row that has seen no key yet)
+                    l[x] += s[x];
+                }
+#pragma unroll
+                for (int x = 0; x < COLS; x += 2) pk[x >> 1] = pack_bf16(s[x], s[x + 1]);
+                wait_pv(sn);  // the last tile's numerators are read
+                // The key's row of P, its 16-byte pieces swizzled by the address bits above the row's.
+                uint8_t* prow = pbuf + key * (2 * kN);
+                const int sw = (key >> 2) & 1;
+                if constexpr (COLS == 4) {
+                    *reinterpret_cast<uint2*>(prow + (sw << 4)) = make_uint2(pk[0], pk[1]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < COLS / 8; ++x)
+                        *reinterpret_cast<uint4*>(prow + ((x ^ sw) << 4)) =
+                            make_uint4(pk[4 * x], pk[4 * x + 1], pk[4 * x + 2], pk[4 * x + 3]);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+                __syncwarp();
+            }
+            // ---- the unit's (or this part's) result: the rows' sums over the threads, then a dim a thread
+            if constexpr (COLS >= 8) {
+                float none[COLS];
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) none[x] = 0.f;
+                transpose_reduce<COLS>(l, none, lane);  // lane: column lane / (32 / COLS)
+                if (lane % (32 / COLS) == 0) red[warp * COLS + lane / (32 / COLS)] = l[0];
+            } else {
+#pragma unroll
+                for (int x = 0; x < COLS; ++x) l[x] = warp_sum(l[x]);
+                if (lane == 0) {
+#pragma unroll
+                    for (int x = 0; x < COLS; ++x) red[warp * COLS + x] = l[x];
+                }
+            }
+            wait_pv(sn);
+            group_bar();
+            float o[COLS];
+            tmem_load<COLS>(tm_o + lane_base, o);
+            tc_fence_before_sync();
+            const bool whole = I.part < 0;
+            float* part = whole ? nullptr : partial_of<kN>(a, blockIdx.x, I.part == 0);
+            const int dim = threadIdx.x;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<long long>(I.q_row) * a.Hq + I.head0) * kHeadDim + dim;
+            int t = 0, h = -1;
+#pragma unroll
+            for (int x = 0; x < COLS; ++x) {
+                if (x >= rows) break;
+                if (++h == p.hp) {
+                    h = 0;
+                    ++t;
+                }
+                const float L = (red[x] + red[COLS + x]) + (red[2 * COLS + x] + red[3 * COLS + x]);
+                if (whole) {
+                    out[(t * a.Hq + h) * kHeadDim] = __float2bfloat16(o[x] * (1.f / L));
+                    if (dim == 0) write_lse<false>(a, I, t, h, ref[x], L);
+                } else {
+                    part[x * 128 + dim] = o[x];
+                    if (dim == 0) {
+                        part[kN * 128 + x] = L == 0.f ? ref[x] : fmaxf(ref[x], -3e38f);  // (only NaN seen: joined)
+                        part[kN * 129 + x] = L;
+                    }
+                }
+            }
+            if (whole) {
+                group_bar();  // red is read
+                continue;
+            }
+            group_bar();
+            if (threadIdx.x == 0) *verdict = last_part(a, I);
+            group_bar();
+            if (!*verdict) continue;
+            // This CTA finished last: it joins the parts, a warp a row; a lane holds a part's weight and, of
+            // the row, four dims.
+            for (int x = warp; x < rows; x += 4) {
+                const int tx = x / p.hp;
+                join_row<kN>(a, I, x, tx, x - tx * p.hp);
+            }
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 54);
+        }
     }
     tc_fence_before_sync();
     __syncthreads();

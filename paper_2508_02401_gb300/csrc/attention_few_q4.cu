@@ -1,332 +1,360 @@
-// Attention of a few query rows a sequence over a paged cache of 4 bits (attention_few.cuh, kv4.cuh).
+// Attention of a few query rows a sequence over a paged cache of 4 bits (attention_common.cuh, kv4.cuh).
 //
-// The cached values are bf16 numbers, so the products are those of the bf16 cache; between the loads and the MMAs, four
-// warps turn the tile's codes into K, a key a lane, in tensor memory (the first operand of S^T = K Q^T), and four into V, a key
-// a row, in shared memory (the first operand of O^T += V^T P, which has the dims on its rows and so cannot come from the
-// lanes of keys).
-#include "attention_few.cuh"
+// A warp takes 16 keys of a tile at a time, straight from the pages into registers, and turns the codes into
+// operands there: S^T [16 keys][8 rows] = K Q^T and O^T [128 dims][8 rows] += V^T P by m16n8k16 MMAs.  The keys of K's
+// fragments and the channels of all of them are taken in the order that makes a thread's share of a row lie together:
+//   K  (rows: keys)      thread (r, c) = (lane / 4, lane % 4): group c of keys 4 (r / 2) + r % 2 and 2 on, 16 bytes of each
+//   Q  (columns: rows)   row r, channels 32 c to 32 c + 31: 64 bytes
+//   V  (rows: channels)  channels 16 r to 16 r + 15 of keys 4 c to 4 c + 3, 8 bytes of each
+// A warp has a softmax of its own (reference, sums, output); the eight of a CTA are joined at a unit's end, the parts of a
+// unit by the CTA that finishes last.
+#include <new>
 #include <string.h>
 
-#include "kv4_loader.cuh"
+#include "attention_common.cuh"
+#include "kv4.cuh"
 
 namespace ckv {
 namespace {
 
-constexpr int kThreadsF4 = 512;
-constexpr int kWarpV = 8, kLoadWarp4 = 12, kMmaWarp4 = 13, kQWarp4 = 14;  // warps 0-3: softmax; 4-7: K; 8-11: V; 15: idle
-constexpr int kRing4 = 6;  // packed tiles of 18 KB
-constexpr int kBuf4 = 3;   // K tiles in tensor memory, V tiles in shared memory
-constexpr int kTmemK4 = 64;   // columns of a K tile, from the first
-constexpr int kTmem4 = 256;   // three K, two S, one O
+constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
+constexpr int kCtas4 = 2;  // on an SM
+constexpr int kRows4 = 16;
+constexpr int kPitch4 = 132;  // floats between the warps' output rows in shared memory
+constexpr float kNoRef = -3e38f;
+static_assert(kTileKeys == 16 * kWarps4, "a tile is a step of every warp");
+static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * kRows4 * 130 <= kAttnPartialFloats, "workspace");
 
-struct FewSmem4 {
-    static constexpr int kV = 0;
-    static constexpr int kQ = kBuf4 * kTileBytes;
-    static constexpr int kP = kQ + 2 * kQBytesF;
-    static constexpr int kRing = kP + kPBytesF;
-    static constexpr int kRed = kRing + kRing4 * kPackedTile;
-    static constexpr int kRef = kRed + kRedBytesF;
-    static constexpr int kItems = kRef + kRefBytesF;
-    static constexpr int kBars = kItems + kAttnItemRing * static_cast<int>(sizeof(Item));
-    static constexpr int kFull = 0, kFree = kFull + kRing4, kKReady = kFree + kRing4, kKFree = kKReady + kBuf4,
-                         kVReady = kKFree + kBuf4, kVFree = kVReady + kBuf4, kQFull = kVFree + kBuf4, kQFree = kQFull + 2,
-                         kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 1, kItemFull = kPvDone + 1,
-                         kItemFree = kItemFull + kAttnItemRing, kDone = kItemFree + kAttnItemRing, kNumBars = kDone + 1;
-    static constexpr int kScan = kBars + 8 * kNumBars;
-    static constexpr int kMisc = kScan + kScanBytes;
-    static constexpr int kBytes = kMisc + 16;
-};
-static_assert(FewSmem4::kBytes <= 232448, "shared memory");
-static_assert(FewSmem4::kRing % 16 == 0 && FewSmem4::kRed % 16 == 0 && kPackedTile % 16 == 0, "alignment");
-
-// A ring of buffers that one side fills and another empties: the current one, and the phase of its barrier.
-template <int N>
-struct Turn {
-    uint32_t at = 0, phase = 0;
-    __device__ void next() {
-        if (++at == N) {
-            at = 0;
-            phase ^= 1;
-        }
-    }
+// One step's bytes of a thread.
+struct Step {
+    uint4 k[2];
+    uint2 v[4];
+    uint32_t ks[2], vs[4];  // scale words
 };
 
-template <int COLS>
-__global__ void __launch_bounds__(kThreadsF4, 1) attention_few_q4_kernel(const __grid_constant__ AttnParams p) {
-    using C = FewSmem4;
-    extern __shared__ __align__(1024) uint8_t sm[];
-    uint8_t* vbuf = sm + C::kV;
-    uint8_t* qbuf = sm + C::kQ;
-    uint8_t* pbuf = sm + C::kP;
-    uint8_t* ring = sm + C::kRing;
-    float* red = reinterpret_cast<float*>(sm + C::kRed);
-    float* ref = reinterpret_cast<float*>(sm + C::kRef);
-    Item* items = reinterpret_cast<Item*>(sm + C::kItems);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(sm + C::kBars);
-    uint64_t* full = bars + C::kFull;
-    uint64_t* freed = bars + C::kFree;
-    uint64_t* k_ready = bars + C::kKReady;
-    uint64_t* k_free = bars + C::kKFree;
-    uint64_t* v_ready = bars + C::kVReady;
-    uint64_t* v_free = bars + C::kVFree;
-    uint64_t* q_full = bars + C::kQFull;
-    uint64_t* q_free = bars + C::kQFree;
-    uint64_t* s_full = bars + C::kSFull;
-    uint64_t* p_full = bars + C::kPFull;
-    uint64_t* pv_done = bars + C::kPvDone;
-    uint64_t* item_full = bars + C::kItemFull;
-    uint64_t* item_free = bars + C::kItemFree;
-    uint64_t* done = bars + C::kDone;
-    long long* scan = reinterpret_cast<long long*>(sm + C::kScan);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + C::kMisc);
-    volatile int* abort = reinterpret_cast<volatile int*>(sm + C::kMisc + 4);
-    volatile int* verdict = reinterpret_cast<volatile int*>(sm + C::kMisc + 8);
-
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const AttnLaunch& a = p.a;
-    const int heads = a.Hkv;            // units of a row tile (a unit has whole KV groups of G = p.hp heads)
-    if ((smem_u32(sm) & 1023u) != 0) {  // the swizzled tiles need an aligned base
-        if (threadIdx.x == 0) record_error(a.status, kDevBadIndex, -2);
-        return;
-    }
-    if (threadIdx.x == 0) {
-        *abort = 0;
-        for (int i = 0; i < kRing4; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&freed[i], 8);  // the warps of K and V
-        }
-        for (int i = 0; i < kBuf4; ++i) {
-            mbar_init(&k_ready[i], 4);
-            mbar_init(&k_free[i], 1);
-            mbar_init(&v_ready[i], 4);
-            mbar_init(&v_free[i], 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], 1);
-            mbar_init(&q_free[i], 1);
-            mbar_init(&s_full[i], 1);
-        }
-        mbar_init(p_full, 4);
-        mbar_init(pv_done, 1);
-        for (int i = 0; i < kAttnItemRing; ++i) {
-            mbar_init(&item_full[i], 1);
-            mbar_init(&item_free[i], 14);  // the warps of the softmax, of K and V, the MMA issuer, the query loader
-        }
-        mbar_init(done, 1);
-        fence_mbar_init();
-    }
-    if (warp == kMmaWarp4) {
-        tmem_alloc(tmem_slot, kTmem4);
-        tmem_relinquish();
-    }
-    // Query rows that a unit does not have are never loaded: zeros (or another unit's rows) in their place.
-    static_assert(C::kP == C::kQ + 2 * kQBytesF, "P follows the query buffers");
-    for (int i = threadIdx.x; i < (2 * kQBytesF + kPBytesF) / 16; i += kThreadsF4)
-        reinterpret_cast<uint4*>(qbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
-    fence_proxy_async_smem();
-    Run run;
-    const bool busy = find_run<kThreadsF4>(p, p.tp, heads, scan, run);
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    if (!busy) {
-        if (warp == kMmaWarp4) tmem_dealloc(*tmem_slot, kTmem4);
-        return;
-    }
-    const uint32_t tm_k = *tmem_slot, tm_s = tm_k + kBuf4 * kTmemK4, tm_o = tm_s + 2 * kN;
-    const long long lim = p.wait_cycles;
-    const FewRoles R{qbuf, pbuf, red, ref, items, item_full, item_free, q_full, q_free, s_full, p_full, pv_done, abort, verdict, tm_s, tm_o};
-    // The next item of a role (a whole warp): false when there is none, or at a wait that gave up (then `ok` is false).
-    auto next_item = [&](int it, Item& I, bool& ok) {
-        const int slot = it % kAttnItemRing;
-        if (!(ok = warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim))) return false;
-        I = items[slot];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&item_free[slot]);
-        __syncwarp();
-        return I.part != kEndItem;
-    };
-
-    if (warp == kLoadWarp4) {
-        // ---------------------------------------------------------------- items, packed tiles
-        Walk walk(p, run, p.tp, heads, scan);
-        PackedLoader<kRing4> tiles{p, ring, full, freed, abort, lim};
-        bool ok = true;
-        for (int it = 0; ok; ++it) {
-            const int slot = it % kAttnItemRing;
-            if (!(ok = warp_wait(&item_free[slot], ((it / kAttnItemRing) & 1) ^ 1, abort, lim))) break;
-            Item I;
-            const bool more = walk.next(I);
-            if (lane == 0) {
-                items[slot] = I;
-                mbar_arrive(&item_full[slot]);
-            }
-            __syncwarp();
-            if (!more) break;
-            ok = tiles.item(I);
-        }
-        if (!ok) {
-            *abort = 1;
-            if (lane == 0) record_error(a.status, kDevTimeout, 61);
-        }
-        tiles.drain();
-        __syncwarp();
-    } else if (warp == kQWarp4) {
-        few_query_role(p, R, lim);
-    } else if (warp == kMmaWarp4) {
-        // ---------------------------------------------------------------- MMA issuer
-        // The logits of a tile before the product of the one before it, as over a bf16 cache.
-        const uint32_t q_addr = desc_addr(qbuf), v_addr = desc_addr(vbuf), p_lo = desc_addr(pbuf) | (1u << 16);
-        Turn<kBuf4> kt, vt;
-        uint32_t sn = 0, pn = 0;  // logits and products issued
-        int it = 0;
-        Item I;
-        bool ok = true, more = next_item(it++, I, ok);
-        auto qk = [&](bool first, bool last) {  // item it - 1
-            const uint32_t qs = (it - 1) & 1;
-            if (first && !warp_wait(&q_full[qs], ((it - 1) >> 1) & 1, abort, lim)) return false;
-            const uint32_t q_lo = uniform((q_addr + qs * (kQBytesF >> 4)) | kDescLoK);
-            const uint32_t d_tmem = uniform(tm_s + (sn & 1) * kN), k_tmem = uniform(tm_k + kt.at * kTmemK4);
-            tile_wait(&k_ready[kt.at], kt.phase, abort, lim, a.status);
-            __syncwarp();
-            tc_fence_after_sync();
-            if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    umma_ts(d_tmem, k_tmem + kk * 8, q_lo + (kk >> 2) * (kN * 128 >> 4) + (kk & 3) * 2, kIdescFewS, kk > 0 ? 1u : 0u);
-                umma_commit(&s_full[sn & 1]);
-                umma_commit(&k_free[kt.at]);
-                if (last) umma_commit(&q_free[qs]);
-            }
-            __syncwarp();
-            kt.next();
-            ++sn;
-            return true;
-        };
-        if (more) ok = qk(true, I.n_tiles == 1);
-        while (ok && more) {
-            const int n = I.n_tiles;
-            for (int i = 0; i < n && ok; ++i) {
-                const bool last = i == n - 1;
-                if (last) {
-                    more = next_item(it++, I, ok);
-                    if (!ok) break;
-                }
-                if (!last && !(ok = qk(false, i + 2 == n))) break;
-                const uint32_t v_lo = uniform((v_addr + vt.at * (kTileBytes >> 4)) | kDescLoV), d_tmem = uniform(tm_o);
-                const uint32_t accumulate = uniform(i > 0);
-                tile_wait(&v_ready[vt.at], vt.phase, abort, lim, a.status);
-                tile_wait(p_full, pn & 1, abort, lim, a.status);
-                ++pn;
-                __syncwarp();
-                tc_fence_after_sync();
-                if (elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        umma_ss<kPHi>(d_tmem, v_lo + kk * (2048 >> 4), p_lo + kk * (2 * kPGroup >> 4), kIdescFewO, kk > 0 ? 1u : accumulate);
-                    umma_commit(pv_done);
-                    umma_commit(&v_free[vt.at]);
-                }
-                __syncwarp();
-                vt.next();
-                if (last && more) ok = qk(true, I.n_tiles == 1);
-            }
-        }
-        if (elect_one()) {
-            if (!ok) {
-                *abort = 1;
-                record_error(a.status, kDevTimeout, 62);
-            }
-            umma_commit(done);
-        }
-        __syncwarp();
-        volatile int never = 0;
-        mbar_wait(done, 0, &never);
-        __syncwarp();
-    } else if (warp < 4) {
-        few_softmax_role<COLS>(p, R, lim);
-    } else if (warp < kLoadWarp4) {
-        // ---------------------------------------------------------------- codes into K and V, a key a thread
-        const bool is_v = warp >= kWarpV;
-        const int key = threadIdx.x & 127;
-        const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        Turn<kRing4> in;
-        Turn<kBuf4> to;
-        bool ok = true, live = true;  // live (a lane's own): none of its waits for a tile gave up
-        Item I;
-        for (int it = 0; next_item(it, I, ok); ++it) {
-            for (int i = 0; i < I.n_tiles; ++i) {
-                live &= tile_wait(&full[in.at], in.phase, abort, lim, a.status);
-                __syncwarp();
-                Kv4Row r = packed_row(ring + in.at * kPackedTile, p.page_shift, key, is_v);
-                __syncwarp();
-                if (lane == 0 && live) mbar_arrive(&freed[in.at]);
-                in.next();
-                tile_wait(is_v ? &v_free[to.at] : &k_free[to.at], to.phase ^ 1, abort, lim, a.status);
-                __syncwarp();
-                if (is_v) {
-                    // Rows behind the sequence's end hold anything, and while their numerators are 0, 0 * NaN is not.
-                    if (key >= I.len - (I.t0 + i) * kTileKeys) {
-                        r.scales = make_uint2(0u, 0u);
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) r.codes[g] = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    uint8_t* row = vbuf + to.at * kTileBytes + key * 128;
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        uint32_t v[16];
-                        kv4_group(r, g, v);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            *reinterpret_cast<uint4*>(row + (g >> 1) * kHalfBytes + ((((g & 1) * 4 + x) ^ (key & 7)) << 4)) =
-                                make_uint4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]);
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&v_ready[to.at]);
-                } else {
-                    tc_fence_after_sync();
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        uint32_t v[16];
-                        kv4_group(r, g, v);
-                        tmem_st16u(tm_k + to.at * kTmemK4 + g * 16 + lane_base, v);
-                    }
-                    tmem_st_wait();
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&k_ready[to.at]);
-                }
-                __syncwarp();
-                to.next();
-            }
-        }
-        if (!ok) {
-            *abort = 1;
-            if (lane == 0) record_error(a.status, kDevTimeout, is_v ? 64 : 63);
-        }
-    }
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    if (warp == kMmaWarp4) tmem_dealloc(*tmem_slot, kTmem4);
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transpose of an 8 x 8 matrix of 16-bit values, a row's pair a thread.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 
-template <int COLS>
+// N8: blocks of 8 rows (1 or 2).
+template <int N8>
+struct FewSmem4 {
+    float o[kWarps4][8 * N8][kPitch4];
+    float m[kWarps4][8 * N8], l[kWarps4][8 * N8];
+    Item items[4];
+    Run run;
+    long long scan[(kScanBytes + 7) / 8];
+    alignas(16) unsigned char walk[sizeof(Walk)];
+    int verdict;
+};
+
+template <int N8>
+__global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(const __grid_constant__ AttnParams p) {
+    extern __shared__ __align__(16) unsigned char sm[];
+    FewSmem4<N8>& S = *reinterpret_cast<FewSmem4<N8>*>(sm);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    const AttnLaunch& a = p.a;
+    const int shift = p.page_shift, heads = a.Hkv;
+    Run run;
+    if (!find_run<kThreads4>(p, p.tp, heads, S.scan, run)) return;
+    if (threadIdx.x == 0) S.run = run;
+    __syncthreads();
+    Walk* walk = reinterpret_cast<Walk*>(S.walk);
+    if (warp == kWarps4 - 1) {  // items, three ahead (a slot is written when every warp is past the item four before)
+        Walk w(p, S.run, p.tp, heads, S.scan);
+        if (lane == 0) {
+            new (walk) Walk(w);
+            for (int i = 0; i < 3; ++i)
+                if (!walk->next(S.items[i])) break;
+        }
+    }
+    __syncthreads();
+
+    // A thread's place in a block of a page: K's and V's codes and scales.
+    const int key = 4 * (r >> 1) + (r & 1);
+    const uint32_t at_k = (((c << shift) + key) << 4), at_ks = (64u << shift) + key * 8 + c * 2;
+    const uint32_t at_v = (72u << shift) + ((((r >> 1) << shift) + 4 * c) << 4) + (r & 1) * 8;
+    const uint32_t at_vs = (136u << shift) + 4 * c * 8 + (r >> 1) * 2;
+
+    auto steps_of = [&](const Item& I) {  // of this warp
+        const int keys = min(I.n_tiles * kTileKeys, I.len - I.t0 * kTileKeys);
+        return (((keys + 15) >> 4) - warp + kWarps4 - 1) / kWarps4;
+    };
+    // The pages of the warp's steps i0 to i0 + 31, a step a lane.
+    auto window = [&](const Item& I, int i0) {
+        const int i = i0 + lane;
+        int page = a.num_pages;
+        if (i < steps_of(I))
+            page = table_page(a, I.seq, a.table + static_cast<size_t>(I.seq) * a.max_blocks, (I.t0 * kTileKeys + (warp + i * kWarps4) * 16) >> shift);
+        return page;
+    };
+    auto load = [&](Step& x, const Item& I, int i, int page) {
+        if (page >= a.num_pages) {  // (reported; the sequence's rows are undefined)
+            x.k[0] = x.k[1] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                x.v[y] = make_uint2(0u, 0u);
+                x.vs[y] = 0u;
+            }
+            x.ks[0] = x.ks[1] = 0u;
+            return;
+        }
+        const int row = (warp + i * kWarps4) * 16 & ((1 << shift) - 1);
+        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            x.k[y] = __ldg(reinterpret_cast<const uint4*>(b + at_k + row * 16 + y * 32));
+            x.ks[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_ks + row * 8 + y * 16));
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            x.v[y] = __ldg(reinterpret_cast<const uint2*>(b + at_v + row * 16 + y * 16));
+            x.vs[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_vs + row * 8 + y * 8));
+        }
+    };
+
+    int now = 0;
+    Step x;
+    {
+        const Item& I = S.items[0];
+        if (I.part == kEndItem) return;
+        now = window(I, 0);
+        if (steps_of(I) > 0) load(x, I, 0, __shfl_sync(0xffffffffu, now, 0));
+    }
+    for (int it = 0;; ++it) {
+        const Item& I = S.items[it & 3];
+        if (I.part == kEndItem) break;
+        const Item& J = S.items[(it + 1) & 3];
+        const int n = steps_of(I), nj = J.part == kEndItem ? 0 : steps_of(J);
+        int ahead = n > 32 ? window(I, 32) : nj > 0 ? window(J, 0) : 0;
+        const int rows = I.ntok * p.hp;
+        // the query rows, as the second operand
+        uint32_t q[N8][16];
+#pragma unroll
+        for (int b = 0; b < N8; ++b) {
+            const int row = b * 8 + r, t = row / p.hp;
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (I.q_row + t) * a.q_tok +
+                                                              (I.head0 + row - t * p.hp) * a.q_head + c * 32);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const uint4 w = row < rows ? __ldg(src + y) : make_uint4(0u, 0u, 0u, 0u);
+                q[b][4 * y] = w.x, q[b][4 * y + 1] = w.y, q[b][4 * y + 2] = w.z, q[b][4 * y + 3] = w.w;
+            }
+        }
+        float ref[N8][2], l[N8][2], o[N8][8][4];
+        int end[N8][2];  // of the columns: the first key that the row does not see
+#pragma unroll
+        for (int b = 0; b < N8; ++b) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                ref[b][e] = kNoRef;
+                l[b][e] = 0.f;
+                end[b][e] = I.pos0 + 1 + (b * 8 + 2 * c + e) / p.hp;
+            }
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) o[b][y][z] = 0.f;
+        }
+        if (n == 0 && nj > 0) {
+            now = ahead;
+            load(x, J, 0, __shfl_sync(0xffffffffu, now, 0));
+        }
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            Step cur = x;
+            if (i + 1 < n) {
+                if (((i + 1) & 31) == 0) {
+                    now = ahead;
+                    ahead = n > i + 33 ? window(I, i + 33) : nj > 0 ? window(J, 0) : 0;
+                }
+                load(x, I, i + 1, __shfl_sync(0xffffffffu, now, (i + 1) & 31));
+            } else if (nj > 0) {
+                now = ahead;
+                load(x, J, 0, __shfl_sync(0xffffffffu, now, 0));
+            }
+            const int k0 = I.t0 * kTileKeys + (warp + i * kWarps4) * 16;
+            // ---- logits
+            float s[N8][4];
+#pragma unroll
+            for (int b = 0; b < N8; ++b)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) s[b][y] = 0.f;
+            {
+                uint32_t s0, z0, s1, z1;
+                kv4_scale(cur.ks[0], s0, z0);
+                kv4_scale(cur.ks[1], s1, z1);
+                const uint32_t wa[4] = {cur.k[0].x, cur.k[0].y, cur.k[0].z, cur.k[0].w};
+                const uint32_t wb[4] = {cur.k[1].x, cur.k[1].y, cur.k[1].z, cur.k[1].w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint4 ka = kv4_word(wa[w], s0, z0), kb = kv4_word(wb[w], s1, z1);
+#pragma unroll
+                    for (int b = 0; b < N8; ++b) {
+                        mma16816(s[b], ka.x, kb.x, ka.y, kb.y, q[b][4 * w], q[b][4 * w + 1]);
+                        mma16816(s[b], ka.z, kb.z, ka.w, kb.w, q[b][4 * w + 2], q[b][4 * w + 3]);
+                    }
+                }
+            }
+            // ---- numerators
+            if (k0 + 16 > I.pos0 + 1) {  // some row does not see some key
+                const int j = k0 + key;
+#pragma unroll
+                for (int b = 0; b < N8; ++b)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (j + (y >> 1) * 2 >= end[b][y & 1]) s[b][y] = -INFINITY;
+                // Rows behind the sequence's end hold anything, and while their numerators are 0, 0 * NaN is not.
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (k0 + 4 * c + y >= I.len) cur.vs[y] = 0u;
+            }
+            float over = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < N8; ++b)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    s[b][y] *= p.c;
+                    over = fmaxf(over, s[b][y] - ref[b][y & 1]);
+                }
+            if (__any_sync(0xffffffffu, over > kAttnTau)) {
+                // Move the references that a key passes by more than 2^8 (or that have none yet).
+#pragma unroll
+                for (int b = 0; b < N8; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(s[b][e], s[b][e + 2]);
+#pragma unroll
+                        for (int y = 4; y < 32; y <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, y));
+                        const bool move = mx - ref[b][e] > kAttnTau;
+                        const float f = move ? ex2_approx(ref[b][e] - mx) : 1.f;
+                        if (move) ref[b][e] = mx;
+                        l[b][e] *= f;
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            o[b][y][e] *= f;
+                            o[b][y][e + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t pb[N8][2];
+#pragma unroll
+            for (int b = 0; b < N8; ++b) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    s[b][y] = ex2_approx(s[b][y] - ref[b][y & 1]);
+                    l[b][y & 1] += s[b][y];
+                }
+                pb[b][0] = transpose8(pack_bf16(s[b][0], s[b][1]));
+                pb[b][1] = transpose8(pack_bf16(s[b][2], s[b][3]));
+            }
+            // ---- output
+            {
+                const uint32_t c01 = __byte_perm(cur.vs[0], cur.vs[1], 0x5410), c23 = __byte_perm(cur.vs[2], cur.vs[3], 0x5410);
+                const uint32_t s01 = c01 & 0xfff0fff0u, s23 = c23 & 0xfff0fff0u;
+                const uint32_t z01 = (c01 & 0x000f000fu) | 0x43004300u, z23 = (c23 & 0x000f000fu) | 0x43004300u;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const uint32_t v0 = w ? cur.v[0].y : cur.v[0].x, v1 = w ? cur.v[1].y : cur.v[1].x;
+                    const uint32_t v2 = w ? cur.v[2].y : cur.v[2].x, v3 = w ? cur.v[3].y : cur.v[3].x;
+                    // even channels of two keys, odd channels
+                    const uint4 e01 = kv4_word(__byte_perm(v0, v1, 0x5410), s01, z01), d01 = kv4_word(__byte_perm(v0, v1, 0x7632), s01, z01);
+                    const uint4 e23 = kv4_word(__byte_perm(v2, v3, 0x5410), s23, z23), d23 = kv4_word(__byte_perm(v2, v3, 0x7632), s23, z23);
+#pragma unroll
+                    for (int b = 0; b < N8; ++b) {
+                        mma16816(o[b][4 * w], e01.x, d01.x, e23.x, d23.x, pb[b][0], pb[b][1]);
+                        mma16816(o[b][4 * w + 1], e01.y, d01.y, e23.y, d23.y, pb[b][0], pb[b][1]);
+                        mma16816(o[b][4 * w + 2], e01.z, d01.z, e23.z, d23.z, pb[b][0], pb[b][1]);
+                        mma16816(o[b][4 * w + 3], e01.w, d01.w, e23.w, d23.w, pb[b][0], pb[b][1]);
+                    }
+                }
+            }
+        }
+        // ---- the unit's (or this part's) result: the warps' outputs side by side, then a warp a row
+#pragma unroll
+        for (int b = 0; b < N8; ++b)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[b][e];
+#pragma unroll
+                for (int y = 4; y < 32; y <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, y);
+                const int row = b * 8 + 2 * c + e;
+                if (row >= rows) continue;
+                if (r == 0) {
+                    S.m[warp][row] = ref[b][e];
+                    S.l[warp][row] = sum;
+                }
+                float4* d = reinterpret_cast<float4*>(&S.o[warp][row][16 * r]);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    d[y] = make_float4(o[b][2 * y][e], o[b][2 * y][e + 2], o[b][2 * y + 1][e], o[b][2 * y + 1][e + 2]);
+            }
+        __syncthreads();
+        if (threadIdx.x == kThreads4 - 32) walk->next(S.items[(it + 3) & 3]);
+        const bool whole = I.part < 0;
+        float* part = whole ? nullptr : partial_of<kRows4>(a, blockIdx.x, I.part == 0);
+        for (int row = warp; row < rows; row += kWarps4) {
+            float wm = lane < kWarps4 ? S.m[lane][row] : kNoRef;
+            const float wl = lane < kWarps4 ? S.l[lane][row] : 0.f;
+            const float M = redux_max(wm);
+            wm = ex2_approx(wm - M);  // (of a warp that saw no key: 0, or 1 for 0 keys)
+            const float L = warp_sum(wm * wl);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int y = 0; y < kWarps4; ++y) {
+                const float f = __shfl_sync(0xffffffffu, wm, y);
+                const float4 v = *reinterpret_cast<const float4*>(&S.o[y][row][4 * lane]);
+                acc.x += v.x * f;
+                acc.y += v.y * f;
+                acc.z += v.z * f;
+                acc.w += v.w * f;
+            }
+            const int t = row / p.hp, h = row - t * p.hp;
+            if (whole) {
+                const float inv = 1.f / L;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + lane * 4;
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                if (lane == 0) write_lse<false>(a, I, t, h, M, L);
+            } else {
+                reinterpret_cast<float4*>(part + row * 128)[lane] = acc;
+                if (lane == 0) {
+                    part[kRows4 * 128 + row] = M;
+                    part[kRows4 * 129 + row] = L;
+                }
+            }
+        }
+        __syncthreads();
+        if (whole) continue;
+        if (threadIdx.x == 0) S.verdict = last_part(a, I);
+        __syncthreads();
+        if (!S.verdict) continue;
+        for (int row = warp; row < rows; row += kWarps4) join_row<kRows4>(a, I, row, row / p.hp, row % p.hp);
+    }
+}
+
+template <int N8>
 cudaError_t launch_few_q4(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
-    auto kern = attention_few_q4_kernel<COLS>;
+    auto kern = attention_few_q4_kernel<N8>;
     static bool configured[kAttnMaxDevices] = {};
-    const cudaError_t e = attn_configure(kern, FewSmem4::kBytes, configured);
+    constexpr int bytes = static_cast<int>(sizeof(FewSmem4<N8>));
+    static_assert(bytes <= 115712, "shared memory of two CTAs");
+    const cudaError_t e = attn_configure(kern, bytes, configured);
     if (e != cudaSuccess) return e;
-    p.hp = p.G;
-    p.tp = COLS / p.G;
-    p.nhb = 1;
-    int grid = device_sm_count();
-    if (grid <= 0) return cudaErrorNoDevice;
-    if (L.max_ctas > 0 && L.max_ctas < grid) grid = L.max_ctas;
+    const int sms = device_sm_count();
+    if (sms <= 0) return cudaErrorNoDevice;
+    int grid = sms * kCtas4;
+    if (L.max_ctas > 0 && L.max_ctas < sms) grid = L.max_ctas;  // (two could go to an SM each)
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
     NvtxRange range("attention_few_q4_kernel");
-    kern<<<grid, kThreadsF4, FewSmem4::kBytes, stream>>>(p);
+    kern<<<grid, kThreads4, bytes, stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -337,13 +365,15 @@ cudaError_t launch_attention_few_q4(const AttnLaunch& L, int rows, cudaStream_t 
     memset(&p, 0, sizeof p);
     p.a = L;
     p.G = L.Hq / L.Hkv;
+    p.hp = p.G;
+    p.tp = (rows <= 8 ? 8 : 16) / p.G;
+    p.nhb = 1;
     p.unit_cost = 2;
     p.min_run = 1;
-    p.page_shift = 0;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
     p.wait_cycles = wait_limit_cycles();
-    return rows <= 4 ? launch_few_q4<4>(L, p, stream) : rows <= 8 ? launch_few_q4<8>(L, p, stream) : launch_few_q4<16>(L, p, stream);
+    return rows <= 8 ? launch_few_q4<1>(L, p, stream) : launch_few_q4<2>(L, p, stream);
 }
 
 }  // namespace ckv
