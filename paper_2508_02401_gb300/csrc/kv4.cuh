@@ -52,12 +52,19 @@ __device__ __forceinline__ void kv4_scale(uint32_t word, uint32_t& s2, uint32_t&
     z2 = __byte_perm(0x4300u | (word & 15u), 0u, 0x1010);
 }
 
+// (w & 0x000f000f) | 0x43004300 in one instruction (the compiler makes two of it).
+__device__ __forceinline__ uint32_t kv4_pair(uint32_t w) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(w));
+    return r;
+}
+
 // The 8 values of a word as four bf16 pairs.  0x4300 | n is 128 + n (bf16 has steps of 1 there); the difference of two
 // such numbers and its product with s are exact.
 __device__ __forceinline__ uint4 kv4_word(uint32_t w, uint32_t s2, uint32_t z2) {
     uint32_t x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = bf16x2_mul(bf16x2_sub(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, z2), s2);
+    for (int i = 0; i < 4; ++i) x[i] = bf16x2_mul(bf16x2_sub(kv4_pair(w >> (4 * i)), z2), s2);
     return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
