@@ -12,29 +12,37 @@
 #include <type_traits>
 
 #include "attention_common.cuh"
+#include "kv4_loader.cuh"
 
 namespace ckv {
 namespace {
 
-constexpr int kThreadsT = 384;
-constexpr int kRingT = 5;  // K and V tiles of 32 KB
+enum Source { kPrompt, kPaged, kPaged4 };  // packed rows, bf16 pages, pages of 4 bits
 constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 0-3, 4-7: softmax; 8, 9: the MMAs of either
+constexpr int kUnpackWarp = 12;              // kPaged4: warps 12-15 make bf16 tiles of the packed ones
 constexpr int kRowsT = 256;
 static_assert(static_cast<size_t>(kAttnTilesCtas) * 2 * kRowsT * 130 <= kAttnPartialFloats, "workspace");
 
+template <Source SRC>
 struct TilesSmem {
-    static constexpr int kQ = kRingT * kTileBytes;
-    static constexpr int kItems = kQ + 2 * kTileBytes;
+    static constexpr bool kQ4 = SRC == kPaged4;
+    static constexpr int kThreads = kQ4 ? 512 : 384;
+    static constexpr int kRing = kQ4 ? 4 : 5;    // K and V tiles of 32 KB
+    static constexpr int kPacked = kQ4 ? 3 : 0;  // packed ones of 9 KB
+    static constexpr int kQ = kRing * kTileBytes;
+    static constexpr int kPackedRing = kQ + 2 * kTileBytes;
+    static constexpr int kItems = kPackedRing + kPacked * kPackedTile;
     static constexpr int kBars = kItems + kAttnItemRing * static_cast<int>(sizeof(Item));
-    static constexpr int kFull = 0, kFree = kFull + kRingT, kQFull = kFree + kRingT, kQFree = kQFull + 2,
+    static constexpr int kFull = 0, kFree = kFull + kRing, kQFull = kFree + kRing, kQFree = kQFull + 2,
                          kSFull = kQFree + 2, kPFull = kSFull + 2, kPvDone = kPFull + 2, kTurn = kPvDone + 2,
                          kItemFull = kTurn + 2, kItemFree = kItemFull + kAttnItemRing,
-                         kPair = kItemFree + kAttnItemRing, kDone = kPair + 1, kNumBars = kDone + 1;
+                         kPair = kItemFree + kAttnItemRing, kDone = kPair + 1, kPackedFull = kDone + 1,
+                         kPackedFree = kPackedFull + kPacked, kNumBars = kPackedFree + kPacked;
     static constexpr int kScan = kBars + 8 * kNumBars;
     static constexpr int kMisc = kScan + kScanBytes;  // TMEM base, abort, verdict
     static constexpr int kBytes = kMisc + 16;
+    static_assert(kBytes <= 232448, "shared memory");
 };
-static_assert(TilesSmem::kBytes <= 232448, "shared memory");
 
 constexpr uint32_t kIdescQk = idesc_bf16_f32(128, 128);
 constexpr uint32_t kIdescPv = idesc_bf16_f32(128, 128) | (1u << 16);  // B with N contiguous
@@ -76,9 +84,11 @@ __device__ __forceinline__ bool pair_sync(uint64_t* bar, uint32_t& phase, volati
     return ok;
 }
 
-template <bool PAGED>
-__global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __grid_constant__ AttnParams p) {
-    using SM = TilesSmem;
+template <Source SRC>
+__global__ void __launch_bounds__(TilesSmem<SRC>::kThreads, 1) attention_tiles_kernel(const __grid_constant__ AttnParams p) {
+    using SM = TilesSmem<SRC>;
+    constexpr bool kQ4 = SM::kQ4;
+    constexpr int kRingT = SM::kRing;
     extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t* ring = sm;
     uint8_t* qbuf = sm + SM::kQ;
@@ -111,8 +121,12 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
     if (threadIdx.x == 0) {
         *abort = 0;
         for (int i = 0; i < kRingT; ++i) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], kQ4 ? 4 : 1);
             mbar_init(&freed[i], 2);  // the MMA issuers
+        }
+        for (int i = 0; i < SM::kPacked; ++i) {
+            mbar_init(&bars[SM::kPackedFull + i], 1);
+            mbar_init(&bars[SM::kPackedFree + i], 4);  // the unpacking warps
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
@@ -124,7 +138,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         }
         for (int i = 0; i < kAttnItemRing; ++i) {
             mbar_init(&item_full[i], 1);
-            mbar_init(&item_free[i], 10);  // softmax warps, MMA issuers
+            mbar_init(&item_free[i], kQ4 ? 14 : 10);  // softmax warps, MMA issuers, unpacking warps
         }
         mbar_init(pair, 8);
         mbar_init(done, 2);
@@ -132,15 +146,17 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
     }
     if (warp == kLoadWarp && lane == 0) {
         tma_prefetch_desc(&p.tmap_q);
-        tma_prefetch_desc(&p.tmap_k);
-        tma_prefetch_desc(&p.tmap_v);
+        if constexpr (!kQ4) {
+            tma_prefetch_desc(&p.tmap_k);
+            tma_prefetch_desc(&p.tmap_v);
+        }
     }
     if (warp == kMmaWarp) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
     Run run;
-    const bool busy = find_run<kThreadsT>(p, tq, heads, scan, run);
+    const bool busy = find_run<SM::kThreads>(p, tq, heads, scan, run);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -207,7 +223,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
             if (has_k) live &= tile_wait(&full[ks], phase_of(kd), abort, lim, a.status);
             if (has_v) live &= tile_wait(&full[vs], phase_of(1), abort, lim, a.status);
             if (do_pv) {
-                if (valid < kTileKeys && clear) clear_rows(ring + vs * kTileBytes, valid, lane);
+                if (!kQ4 && valid < kTileKeys && clear) clear_rows(ring + vs * kTileBytes, valid, lane);
                 tile_wait(&p_full[X], pn & 1, abort, lim, a.status);
                 ++pn;
             }
@@ -277,13 +293,65 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         __syncwarp();
     };
 
-    if (warp >= kMmaWarp) {
-        // 384 threads * 168 = 128 * 72 + 256 * 216 registers
-        setmaxnreg_dec<72>();
+    if (kQ4 && warp >= kUnpackWarp) {
+        // ---------------------------------------------------------------- packed tiles into bf16 tiles, a key a thread
+        setmaxnreg_dec<64>();
+        uint8_t* packed = sm + SM::kPackedRing;
+        const int key = threadIdx.x & 127;
+        uint32_t in = 0, in_phase = 0, to = 0, to_phase = 1;
+        bool ok = true, live = true;  // live (a lane's own): none of its waits for a packed tile gave up
+        for (int it = 0; ok; ++it) {
+            const int slot = it % kAttnItemRing;
+            if (!(ok = warp_wait(&item_full[slot], (it / kAttnItemRing) & 1, abort, lim))) break;
+            const int n = items[slot].n_tiles, keys = items[slot].len - items[slot].t0 * kTileKeys, part = items[slot].part;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&item_free[slot]);
+            __syncwarp();
+            if (part == kEndItem) break;
+            for (int u = 0; u < 2 * n; ++u) {  // K and V of each tile
+                live &= tile_wait(&bars[SM::kPackedFull + in], in_phase, abort, lim, a.status);
+                __syncwarp();
+                Kv4Row r = kv4_row(packed + in * kPackedTile + static_cast<uint32_t>(key >> p.page_shift) * (kKv4RowBytes << p.page_shift),
+                                   p.page_shift, key & ((1 << p.page_shift) - 1));
+                // (the reads before the copy that goes over them: without this fence the next copy overtook some)
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0 && live) mbar_arrive(&bars[SM::kPackedFree + in]);
+                if (++in == SM::kPacked) {
+                    in = 0;
+                    in_phase ^= 1;
+                }
+                // Rows behind the sequence's end hold anything, and while their numerators are 0, 0 * NaN is not.
+                if (key >= keys - (u >> 1) * kTileKeys) r.scales = make_uint2(0u, 0u);
+                tile_wait(&freed[to], to_phase, abort, lim, a.status);
+                __syncwarp();
+                unpack_row(r, ring + to * kTileBytes, key);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&full[to]);
+                __syncwarp();
+                if (++to == kRingT) {
+                    to = 0;
+                    to_phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {
+            *abort = 1;
+            if (lane == 0) record_error(a.status, kDevTimeout, 46);
+        }
+    } else if (warp >= kMmaWarp) {
+        // 384 threads * 168 = 128 * 72 + 256 * 216 registers; kPaged4: 512 * 128 = 128 * (64 + 64) + 256 * 192
+        setmaxnreg_dec<kQ4 ? 64 : 72>();
         if (warp == kLoadWarp) {
             // ------------------------------------------------------------ items, query rows, K and V tiles
             Walk walk(p, run, tq, heads, scan);
-            TileLoader<PAGED, kRingT> tiles{p, ring, full, freed, abort, lim};
+            auto tiles = [&] {
+                if constexpr (kQ4)
+                    return PackedLoader<SM::kPacked>{p, sm + SM::kPackedRing, bars + SM::kPackedFull, bars + SM::kPackedFree, abort, lim};
+                else
+                    return TileLoader<SRC == kPaged, kRingT>{p, ring, full, freed, abort, lim};
+            }();
             uint32_t qn0 = 0, qn1 = 0;
             bool ok = true;
             for (int it = 0; ok; ++it) {
@@ -335,7 +403,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
         }
     } else {
         // ---------------------------------------------------------------- softmax, a row a thread
-        setmaxnreg_inc<216>();
+        setmaxnreg_inc<kQ4 ? 192 : 216>();
         const int X = warp >> 2, r = threadIdx.x & 127, row = threadIdx.x;
         const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t s_tmem = kTmS + X * 128 + lane_base, o_tmem = kTmO + X * 128 + lane_base;
@@ -468,7 +536,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                 }
             }
             if (whole) {
-                if (valid) write_lse<!PAGED>(a, I, tok, h_r, mc, l);
+                if (valid) write_lse<SRC == kPrompt>(a, I, tok, h_r, mc, l);
                 continue;
             }
             if (valid) {
@@ -517,7 +585,7 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
                     store_bf16(out + q4 + x, pk, wide);
                 }
             }
-            write_lse<!PAGED>(a, I, tok, h_r, M, L);
+            write_lse<SRC == kPrompt>(a, I, tok, h_r, M, L);
         }
         if (!ok) {
             *abort = 1;
@@ -530,14 +598,14 @@ __global__ void __launch_bounds__(kThreadsT, 1) attention_tiles_kernel(const __g
     if (warp == kMmaWarp) tmem_dealloc(*tmem_slot, 512);
 }
 
-template <bool PAGED>
+template <Source SRC>
 cudaError_t launch_variant(const AttnParams& p, int grid, cudaStream_t stream) {
-    auto kern = attention_tiles_kernel<PAGED>;
+    auto kern = attention_tiles_kernel<SRC>;
     static bool configured[kAttnMaxDevices] = {};
-    const cudaError_t e = attn_configure(kern, TilesSmem::kBytes, configured);
+    const cudaError_t e = attn_configure(kern, TilesSmem<SRC>::kBytes, configured);
     if (e != cudaSuccess) return e;
     NvtxRange range("attention_tiles_kernel");
-    kern<<<grid, kThreadsT, TilesSmem::kBytes, stream>>>(p);
+    kern<<<grid, TilesSmem<SRC>::kThreads, TilesSmem<SRC>::kBytes, stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -568,7 +636,8 @@ cudaError_t launch_attention_tiles(const AttnLaunch& L, const CUtensorMap& map_q
     if (grid <= 0) return cudaErrorNoDevice;
     if (L.max_ctas > 0 && L.max_ctas < grid) grid = L.max_ctas;
     if (grid > kAttnTilesCtas) grid = kAttnTilesCtas;
-    return L.paged ? launch_variant<true>(p, grid, stream) : launch_variant<false>(p, grid, stream);
+    return L.q4 ? launch_variant<kPaged4>(p, grid, stream)
+           : L.paged ? launch_variant<kPaged>(p, grid, stream) : launch_variant<kPrompt>(p, grid, stream);
 }
 
 }  // namespace ckv

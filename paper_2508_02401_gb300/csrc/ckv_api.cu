@@ -1716,7 +1716,7 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // among idle sequences (256 tokens, 255 idle: 692 / 49).
     const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
     const bool few = L.paged && rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64);
-    CUtensorMap mq, mk, mv;
+    CUtensorMap mq, mk{}, mv{};  // (a cache of 4 bits has no maps)
     ckv_status st;
     if (!few) {
         const int hp = attn_heads_per_tile(L.Hq, L.Hkv), tp = kTileKeys / hp;
@@ -1724,7 +1724,7 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
         const int box[3] = {64, hp, tp};
         if ((st = make_rows_map(&mq, L.q, 3, dims, strides, box))) return st;
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 2 && !L.q4; ++i) {
         const void* ptr = i ? L.v : L.k;
         CUtensorMap* map = i ? &mv : &mk;
         if (L.paged) {
@@ -1739,7 +1739,9 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
         }
         if (st) return st;
     }
-    const cudaError_t e = few ? launch_attention_few(L, mk, mv, static_cast<int>(rows), stream) : launch_attention_tiles(L, mq, mk, mv, stream);
+    const cudaError_t e = !few ? launch_attention_tiles(L, mq, mk, mv, stream)
+                          : L.q4 ? launch_attention_few_q4(L, static_cast<int>(rows), stream)
+                                 : launch_attention_few(L, mk, mv, static_cast<int>(rows), stream);
     return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
 }
 
@@ -1890,14 +1892,11 @@ ckv_status ckv_paged_attention_q4(const ckv_config* cfg, const ckv_paged_cache_q
                                    workspace_bytes, L)))
         return st;
     if (num_tokens == 0) return CKV_OK;
+    L.q4 = true;
     L.k = cache->pages;
     L.page_stride = page_stride;
     L.num_pages = cache->num_pages;
-    const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
-    const bool few = rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64);
-    const cudaError_t e = few ? launch_attention_few_q4(L, static_cast<int>(rows), reinterpret_cast<cudaStream_t>(stream))
-                              : launch_attention_q4(L, reinterpret_cast<cudaStream_t>(stream));
-    return e == cudaSuccess ? CKV_OK : cuda_fail(e, "launching the attention kernel");
+    return enqueue_attention(L, reinterpret_cast<cudaStream_t>(stream));
 }
 
 ckv_status ckv_block_tables(int32_t page_size, int32_t num_rows, const int32_t* cache_lens,

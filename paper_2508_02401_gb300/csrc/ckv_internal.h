@@ -220,6 +220,7 @@ struct AttnLaunch {
     const int32_t* cu;              // device [S+1]: query rows of each sequence, from cu[0]
     const int32_t* lens;            // device [S]: keys of each sequence (null: its query rows)
     bool paged;
+    bool q4;                        // k are the pages of a cache of 4 bits, page_stride is in bytes
     int64_t page_stride;            // elements between pages; a page is [page_size, H_kv, 128]
     int page_size, num_pages, max_blocks;
     const int32_t* table;           // device [S][max_blocks]
@@ -298,9 +299,7 @@ struct AppendLaunch {
 long long append_blocks(int T, int Hq, int Hkv);  // CTAs (Hq: 0 without queries)
 cudaError_t launch_cache_append(const AppendLaunch& L, cudaStream_t stream);
 
-// Attention over a cache of 4 bits: AttnLaunch::k are its pages, page_stride is in bytes.
-cudaError_t launch_attention_q4(const AttnLaunch& L, cudaStream_t stream);
-// Units of 4, 8 or 16 rows, as launch_attention_few (attention_few_q4.cu).
+// Over a cache of 4 bits (AttnLaunch::q4), units of 8 or 16 rows, as launch_attention_few (attention_few_q4.cu).
 cudaError_t launch_attention_few_q4(const AttnLaunch& L, int rows, cudaStream_t stream);
 
 int device_sm_count();

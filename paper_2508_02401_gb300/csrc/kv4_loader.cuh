@@ -1,4 +1,5 @@
-// Tiles of 128 cached rows in 4 bits, from the pages into a ring of shared memory.
+// Tiles of 128 cached rows in 4 bits, from the pages into a ring of shared memory and from there, as bf16, into the tiles
+// that the MMAs read.
 #pragma once
 
 #include "attention_common.cuh"
@@ -7,7 +8,8 @@
 namespace ckv {
 namespace {
 
-constexpr int kPackedTile = 2 * kKv4RowBytes * kTileKeys;  // K and V of 128 tokens of a head: 18 KB
+constexpr int kPackedTile = kKv4RowBytes * kTileKeys;  // K or V of 128 tokens of a head: 9 KB
+static_assert(kPackedTile % 16 == 0, "alignment");
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
@@ -15,8 +17,9 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  : "memory");
 }
 
-// One warp loads an item's tiles into the ring, a page a lane: a head's K and V of a page lie together, so a page is
-// one copy (a multiple of 2304 bytes at such an offset: the 16-byte rule of copies holds for any page size).
+// One warp loads an item's packed tiles into the ring: K0 V0 K1 V1 ..., a page a lane (its block of K or V is one copy:
+// a multiple of 1152 bytes at such an offset, so the 16-byte rule of copies holds for any page size).  A page that is out of
+// range is not loaded.
 template <int RING>
 struct PackedLoader {
     const AttnParams& p;
@@ -27,18 +30,18 @@ struct PackedLoader {
     long long lim;
     uint32_t slot = 0, phase = 1, use = 0;
 
-    __device__ bool load(const Item& I, int page, int first) {
+    __device__ bool load(const Item& I, int page, int first, int v) {
         if (!warp_wait(&freed[slot], phase, abort, lim)) return false;
         const AttnLaunch& a = p.a;
         const int lane = threadIdx.x & 31;
-        const uint32_t bytes = (2 * kKv4RowBytes) << p.page_shift;
+        const uint32_t bytes = kKv4RowBytes << p.page_shift;
         const bool mine = lane >= first && lane < first + (kTileKeys >> p.page_shift) && page < a.num_pages;
         const uint32_t pages = __popc(__ballot_sync(0xffffffffu, mine));
         if (lane == 0) mbar_arrive_expect_tx(&full[slot], pages * bytes);
         __syncwarp();
         if (mine)
             bulk_load(ring + slot * kPackedTile + (lane - first) * bytes,
-                      static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * bytes, bytes, &full[slot]);
+                      static_cast<const uint8_t*>(a.k) + page * a.page_stride + (2ll * I.g + v) * bytes, bytes, &full[slot]);
         __syncwarp();
         ++use;
         if (++slot == RING) {
@@ -65,7 +68,8 @@ struct PackedLoader {
                 now = ahead;
                 ahead = window(u + per);
             }
-            if (!load(I, now, (u & (per - 1)) << ppt_shift)) return false;
+            const int first = (u & (per - 1)) << ppt_shift;
+            if (!load(I, now, first, 0) || !load(I, now, first, 1)) return false;
         }
         return true;
     }
@@ -77,10 +81,18 @@ struct PackedLoader {
     }
 };
 
-// The block of a tile's row (a key of the tile), and the row in its page.
-__device__ __forceinline__ Kv4Row packed_row(const uint8_t* tile, int shift, int key, bool v) {
-    const uint8_t* block = tile + (static_cast<uint32_t>(key >> shift) * 2 + (v ? 1 : 0)) * (kKv4RowBytes << shift);
-    return kv4_row(block, shift, key & ((1 << shift) - 1));
+// Row `key` of a packed tile into a tile of 64-dim halves, 128 keys of 128 bytes with the 128-byte swizzle.
+__device__ __forceinline__ void unpack_row(const Kv4Row& r, uint8_t* tile, int key) {
+    uint8_t* row = tile + key * 128;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        uint32_t v[16];
+        kv4_group(r, g, v);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<uint4*>(row + (g >> 1) * kHalfBytes + ((((g & 1) * 4 + x) ^ (key & 7)) << 4)) =
+                make_uint4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]);
+    }
 }
 
 }  // namespace
