@@ -19,6 +19,8 @@ namespace {
 constexpr int kAppThreads = 256;
 constexpr int kAppToks = kAppThreads / 16;  // tokens of a CTA
 constexpr int kAppQ = 4, kAppKv = 2;        // query heads, KV heads (a row of K and one of V each) of a half-warp
+constexpr int kAppRows = 4;
+static_assert(kAppQ == kAppRows && 2 * kAppKv == kAppRows, "rows of a half-warp");
 
 enum { kRotNone = 0, kRotHalves = 1, kRotPairs = 2 };
 
@@ -63,9 +65,18 @@ __device__ __forceinline__ void load_angles(const AppendLaunch& p, int pos, int 
     }
 }
 
-// A lane's 8 channels of a row, rotated (a whole half-warp).  The fp32 result r is off by 2^-24 (|y s| + |r|) at most;
-// where all of a wider interval rounds to one bf16 number, that is the result, otherwise (1 element in 2000) the sum is
-// taken in 64 bits, where both products are exact.
+// a c + b s to the last bit of 32: the products' and the sum's rounding errors (exact by fused operations and the known
+// error of a sum of two) are added at the end.
+__device__ __forceinline__ float turn_exact(float a, float c, float b, float s) {
+    // (intrinsics: the compiler would fuse a product with a sum)
+    const float p = __fmul_rn(a, c), q = __fmul_rn(b, s), pe = fmaf(a, c, -p), qe = fmaf(b, s, -q);
+    const float r = __fadd_rn(p, q), t = __fadd_rn(r, -p), e = __fadd_rn(__fadd_rn(p, -__fadd_rn(r, -t)), __fadd_rn(q, -t));
+    return fabsf(r) <= FLT_MAX ? __fadd_rn(r, __fadd_rn(e, __fadd_rn(pe, qe))) : r;
+}
+
+// A lane's 8 channels of a row, rotated (a whole half-warp).  The fp32 result r = a c + q, q = b s, is off by 2^-24 (|q| + |r|)
+// at most; where all numbers so near round to one bf16 number, that is the result (roundings keep the order of
+// numbers), otherwise (one pair in 2000) the sum is taken exactly.
 template <int ROT>
 __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
     const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
@@ -87,8 +98,8 @@ __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
             const float xf = e ? bf16_hi(x[i]) : bf16_lo(x[i]), yf = e ? bf16_hi(y[i]) : bf16_lo(y[i]);
             const float q = yf * A.s[2 * i + e], r = fmaf(xf, A.c[2 * i + e], q);
             const float w = fabsf(q) + fabsf(r);
-            l[e] = fmaf(w, -0x1p-23f, r);
-            h[e] = fmaf(w, 0x1p-23f, r);
+            l[e] = fmaf(w, -0x1.00001p-24f, r);
+            h[e] = fmaf(w, 0x1.00001p-24f, r);
         }
         lo[i] = pack_bf16x2(l[0], l[1]);
         hi[i] = pack_bf16x2(h[0], h[1]);
@@ -96,26 +107,36 @@ __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
     }
     if (differ) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float r[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const double xd = e ? bf16_hi(x[i]) : bf16_lo(x[i]), yd = e ? bf16_hi(y[i]) : bf16_lo(y[i]);
-                r[e] = static_cast<float>(fma(xd, static_cast<double>(A.c[2 * i + e]), yd * static_cast<double>(A.s[2 * i + e])));
-            }
-            lo[i] = pack_bf16x2(r[0], r[1]);
-        }
+        for (int i = 0; i < 4; ++i)
+            if (lo[i] != hi[i])
+                lo[i] = pack_bf16x2(turn_exact(bf16_lo(x[i]), A.c[2 * i], bf16_lo(y[i]), A.s[2 * i]),
+                                    turn_exact(bf16_hi(x[i]), A.c[2 * i + 1], bf16_hi(y[i]), A.s[2 * i + 1]));
     }
     return make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
 template <bool Q4, int ROT>
-__global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_constant__ AppendLaunch p) {
+__global__ void __launch_bounds__(kAppThreads, 4) cache_append_kernel(const __grid_constant__ AppendLaunch p) {
     const int c = threadIdx.x & 15;
     const int nq = p.q ? (p.Hq + kAppQ - 1) / kAppQ : 0, chunks = nq + (p.Hkv + kAppKv - 1) / kAppKv;
     const int block = blockIdx.x / chunks, ch = blockIdx.x - block * chunks;
     const int t = block * kAppToks + static_cast<int>(threadIdx.x >> 4);
     bool live = t < p.T;
+    // Every load that does not wait for another goes first: the rows, the position, the slot.
+    const bool query = ROT != kRotNone && ch < nq;
+    const int h0 = query ? ch * kAppQ : (ch - nq) * kAppKv;
+    uint4 x[kAppRows];  // queries, or K and V of each head
+#pragma unroll
+    for (int u = 0; u < kAppRows; ++u) {
+        const int h = query ? h0 + u : h0 + (u >> 1);
+        const bool v = u & 1;
+        x[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && h < (query ? p.Hq : p.Hkv)) {
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(query ? p.q : v ? p.v : p.k);
+            x[u] = *reinterpret_cast<const uint4*>(src + (query ? t * p.q_tok + h * p.q_head : t * p.tok_stride + h * p.head_stride) + c * 8);
+        }
+    }
+    int slot = live && !query ? p.slots[t] : -1;
     Angles A;
     if constexpr (ROT != kRotNone) {
         const int pos = live ? p.positions[t] : -1;
@@ -125,16 +146,7 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_
         }
         load_angles<ROT>(p, pos, c, live, A);
     }
-    if (ch < nq) {
-        const int h0 = ch * kAppQ;
-        uint4 x[kAppQ];
-#pragma unroll
-        for (int u = 0; u < kAppQ; ++u) {
-            x[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (live && h0 + u < p.Hq)
-                x[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + t * p.q_tok +
-                                                       (h0 + u) * p.q_head + c * 8);
-        }
+    if (query) {
 #pragma unroll
         for (int u = 0; u < kAppQ; ++u) {
             if constexpr (ROT != kRotNone) x[u] = rotate8<ROT>(x[u], A);
@@ -144,18 +156,7 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_
         }
         return;
     }
-    const int h0 = (ch - nq) * kAppKv;
-    uint4 k[kAppKv], v[kAppKv];
-#pragma unroll
-    for (int u = 0; u < kAppKv; ++u) {
-        k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (live && h0 + u < p.Hkv) {
-            const long long src = t * p.tok_stride + (h0 + u) * p.head_stride + c * 8;
-            k[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k) + src);
-            v[u] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v) + src);
-        }
-    }
-    int slot = live ? p.slots[t] : -1;
+    if (!live) slot = -1;
     if (slot < -1 || slot >= p.num_slots) {
         if (c == 0 && h0 == 0) record_error(p.status, kDevBadIndex, t);
         slot = -1;
@@ -164,11 +165,13 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_
     const int row = slot & ((1 << p.shift) - 1);
 #pragma unroll
     for (int u = 0; u < kAppKv; ++u) {
-        if constexpr (ROT != kRotNone) k[u] = rotate8<ROT>(k[u], A);
+        uint4 k = x[2 * u];
+        const uint4 v = x[2 * u + 1];
+        if constexpr (ROT != kRotNone) k = rotate8<ROT>(k, A);
         const bool has = live && h0 + u < p.Hkv;
         const long long to = (static_cast<long long>(t) * p.Hkv + h0 + u) * kHeadDim + c * 8;
         if constexpr (Q4) {
-            const Kv4Lane kq = kv4_quantise(k[u]), vq = kv4_quantise(v[u]);
+            const Kv4Lane kq = kv4_quantise(k), vq = kv4_quantise(v);
             if (has && slot >= 0) {
                 uint8_t* d = static_cast<uint8_t*>(p.k_pages) + page * p.page_stride +
                              (static_cast<long long>(h0 + u) << p.shift) * (2 * kKv4RowBytes);
@@ -180,10 +183,10 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const __grid_
         } else {
             if (has && slot >= 0) {
                 const long long d = page * p.page_stride + (static_cast<long long>(row) * p.Hkv + h0 + u) * kHeadDim + c * 8;
-                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_pages) + d) = k[u];
-                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.v_pages) + d) = v[u];
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_pages) + d) = k;
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.v_pages) + d) = v;
             }
-            if (has && p.k_out) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_out) + to) = k[u];
+            if (has && p.k_out) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.k_out) + to) = k;
         }
     }
 }
