@@ -60,7 +60,7 @@ template <int N8>
 __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(const __grid_constant__ AttnParams p) {
     extern __shared__ __align__(16) unsigned char sm[];
     FewSmem4<N8>& S = *reinterpret_cast<FewSmem4<N8>*>(sm);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     const AttnLaunch& a = p.a;
     const int shift = p.page_shift, heads = a.Hkv;
     Run run;
@@ -107,17 +107,19 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
             x.ks[0] = x.ks[1] = 0u;
             return;
         }
+        // (a uniform base, and the thread's places in 32 bits)
         const int row = (warp + i * kWarps4) * 16 & ((1 << shift) - 1);
-        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift);
+        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift) + row * 8;
+        const uint8_t* b2 = b + row * 8;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-            x.k[y] = __ldg(reinterpret_cast<const uint4*>(b + at_k + row * 16 + y * 32));
-            x.ks[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_ks + row * 8 + y * 16));
+            x.k[y] = __ldg(reinterpret_cast<const uint4*>(b2 + at_k + y * 32));
+            x.ks[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_ks + y * 16));
         }
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            x.v[y] = __ldg(reinterpret_cast<const uint2*>(b + at_v + row * 16 + y * 16));
-            x.vs[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_vs + row * 8 + y * 8));
+            x.v[y] = __ldg(reinterpret_cast<const uint2*>(b2 + at_v + y * 16));
+            x.vs[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_vs + y * 8));
         }
     };
 
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
         const Item& I = S.items[0];
         if (I.part == kEndItem) return;
         now = window(I, 0);
-        if (steps_of(I) > 0) load(x, I, 0, __shfl_sync(0xffffffffu, now, 0));
+        if (steps_of(I) > 0) load(x, I, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
     }
     for (int it = 0;; ++it) {
         const Item& I = S.items[it & 3];
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
         }
         if (n == 0 && nj > 0) {
             now = ahead;
-            load(x, J, 0, __shfl_sync(0xffffffffu, now, 0));
+            load(x, J, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
         }
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
@@ -176,10 +178,10 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                     now = ahead;
                     ahead = n > i + 33 ? window(I, i + 33) : nj > 0 ? window(J, 0) : 0;
                 }
-                load(x, I, i + 1, __shfl_sync(0xffffffffu, now, (i + 1) & 31));
+                load(x, I, i + 1, uniform(__shfl_sync(0xffffffffu, now, (i + 1) & 31)));
             } else if (nj > 0) {
                 now = ahead;
-                load(x, J, 0, __shfl_sync(0xffffffffu, now, 0));
+                load(x, J, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
             }
             const int k0 = I.t0 * kTileKeys + (warp + i * kWarps4) * 16;
             // ---- logits
@@ -217,13 +219,13 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 for (int y = 0; y < 4; ++y)
                     if (k0 + 4 * c + y >= I.len) cur.vs[y] = 0u;
             }
-            float over = -INFINITY;
+            float x2[N8][4], over = -INFINITY;  // the logits over their references
 #pragma unroll
             for (int b = 0; b < N8; ++b)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    s[b][y] *= p.c;
-                    over = fmaxf(over, s[b][y] - ref[b][y & 1]);
+                    x2[b][y] = fmaf(s[b][y], p.c, -ref[b][y & 1]);
+                    over = fmaxf(over, x2[b][y]);
                 }
             if (__any_sync(0xffffffffu, over > kAttnTau)) {
                 // Move the references that a key passes by more than 2^8 (or that have none yet).
@@ -231,12 +233,14 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 for (int b = 0; b < N8; ++b)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[b][e], s[b][e + 2]);
+                        float mx = fmaxf(s[b][e], s[b][e + 2]) * p.c;
 #pragma unroll
                         for (int y = 4; y < 32; y <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, y));
                         const bool move = mx - ref[b][e] > kAttnTau;
                         const float f = move ? ex2_approx(ref[b][e] - mx) : 1.f;
                         if (move) ref[b][e] = mx;
+                        x2[b][e] = fmaf(s[b][e], p.c, -ref[b][e]);
+                        x2[b][e + 2] = fmaf(s[b][e + 2], p.c, -ref[b][e]);
                         l[b][e] *= f;
 #pragma unroll
                         for (int y = 0; y < 8; ++y) {
@@ -250,11 +254,11 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
             for (int b = 0; b < N8; ++b) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    s[b][y] = ex2_approx(s[b][y] - ref[b][y & 1]);
-                    l[b][y & 1] += s[b][y];
+                    x2[b][y] = ex2_approx(x2[b][y]);
+                    l[b][y & 1] += x2[b][y];
                 }
-                pb[b][0] = transpose8(pack_bf16(s[b][0], s[b][1]));
-                pb[b][1] = transpose8(pack_bf16(s[b][2], s[b][3]));
+                pb[b][0] = transpose8(pack_bf16(x2[b][0], x2[b][1]));
+                pb[b][1] = transpose8(pack_bf16(x2[b][2], x2[b][3]));
             }
             // ---- output
             {

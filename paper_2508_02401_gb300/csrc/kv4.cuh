@@ -46,17 +46,18 @@ __device__ __forceinline__ uint32_t bf16x2_max_nan(uint32_t a, uint32_t b) {
     return r;
 }
 
-// A scale word's pair (s, s) and pair (128 + z, 128 + z) in bf16.
-__device__ __forceinline__ void kv4_scale(uint32_t word, uint32_t& s2, uint32_t& z2) {
-    s2 = __byte_perm(word & 0xfff0u, 0u, 0x1010);
-    z2 = __byte_perm(0x4300u | (word & 15u), 0u, 0x1010);
-}
-
 // (w & 0x000f000f) | 0x43004300 in one instruction (the compiler makes two of it).
 __device__ __forceinline__ uint32_t kv4_pair(uint32_t w) {
     uint32_t r;
     asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(w));
     return r;
+}
+
+// A scale word's pair (s, s) and pair (128 + z, 128 + z) in bf16.
+__device__ __forceinline__ void kv4_scale(uint32_t word, uint32_t& s2, uint32_t& z2) {
+    const uint32_t both = __byte_perm(word, 0u, 0x1010);
+    s2 = both & 0xfff0fff0u;
+    z2 = kv4_pair(both);
 }
 
 // The 8 values of a word as four bf16 pairs.  0x4300 | n is 128 + n (bf16 has steps of 1 there); the difference of two
