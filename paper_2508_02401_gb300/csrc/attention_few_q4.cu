@@ -17,12 +17,10 @@
 namespace ckv {
 namespace {
 
-constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
 constexpr int kCtas4 = 2;  // on an SM
 constexpr int kRows4 = 16;
 constexpr int kPitch4 = 132;  // floats between the warps' output rows in shared memory
 constexpr float kNoRef = -3e38f;
-static_assert(kTileKeys == 16 * kWarps4, "a tile is a step of every warp");
 static_assert(static_cast<size_t>(kAttnMaxCtas) * 2 * kRows4 * 130 <= kAttnPartialFloats, "workspace");
 
 // One step's bytes of a thread.
@@ -47,8 +45,10 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 // N8: blocks of 8 rows (1 or 2).
 template <int N8>
 struct FewSmem4 {
-    float o[kWarps4][8 * N8][kPitch4];
-    float m[kWarps4][8 * N8], l[kWarps4][8 * N8];
+    static constexpr int kWarps4 = N8 == 1 ? 8 : 6;  // (two CTAs of 168 registers a thread: 40 sequences, 14 rows each, 49 us, one CTA of 12 warps 57)
+    static constexpr int kBufs = N8 == 1 ? 2 : 1;  // of the warps' outputs (two: no barrier after they are read)
+    float o[kBufs][kWarps4][8 * N8][kPitch4];
+    float m[kBufs][kWarps4][8 * N8], l[kBufs][kWarps4][8 * N8];
     Item items[4];
     Run run;
     long long scan[(kScanBytes + 7) / 8];
@@ -57,7 +57,8 @@ struct FewSmem4 {
 };
 
 template <int N8>
-__global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_few_q4_kernel(const __grid_constant__ AttnParams p) {
+    constexpr int kWarps4 = FewSmem4<N8>::kWarps4, kThreads4 = 32 * kWarps4;
     extern __shared__ __align__(16) unsigned char sm[];
     FewSmem4<N8>& S = *reinterpret_cast<FewSmem4<N8>*>(sm);
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
@@ -72,11 +73,11 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
         Walk w(p, S.run, p.tp, heads, S.scan);
         if (lane == 0) {
             new (walk) Walk(w);
-            for (int i = 0; i < 3; ++i)
-                if (!walk->next(S.items[i])) break;
+            if (walk->next(S.items[0])) walk->next(S.items[1]);
         }
     }
     __syncthreads();
+    if (threadIdx.x == kThreads4 - 32 && S.items[0].part != kEndItem) walk->next(S.items[2]);  // (read after the next barrier)
 
     // A thread's place in a block of a page: K's and V's codes and scales.
     const int key = 4 * (r >> 1) + (r & 1);
@@ -150,6 +151,9 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 const uint4 w = row < rows ? __ldg(src + y) : make_uint4(0u, 0u, 0u, 0u);
                 q[b][4 * y] = w.x, q[b][4 * y + 1] = w.y, q[b][4 * y + 2] = w.z, q[b][4 * y + 3] = w.w;
             }
+            if (J.part != kEndItem && t < J.ntok)  // the next item's, so that they are near then
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(static_cast<const __nv_bfloat16*>(a.q) + (J.q_row + t) * a.q_tok +
+                                                              (J.head0 + row - t * p.hp) * a.q_head + c * 32));
         }
         float ref[N8][2], l[N8][2], o[N8][8][4];
         int end[N8][2];  // of the columns: the first key that the row does not see
@@ -282,6 +286,7 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 }
             }
         }
+        const int buf = it & (FewSmem4<N8>::kBufs - 1);
         // ---- the unit's (or this part's) result: the warps' outputs side by side, then a warp a row
 #pragma unroll
         for (int b = 0; b < N8; ++b)
@@ -293,10 +298,10 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 const int row = b * 8 + 2 * c + e;
                 if (row >= rows) continue;
                 if (r == 0) {
-                    S.m[warp][row] = ref[b][e];
-                    S.l[warp][row] = sum;
+                    S.m[buf][warp][row] = ref[b][e];
+                    S.l[buf][warp][row] = sum;
                 }
-                float4* d = reinterpret_cast<float4*>(&S.o[warp][row][16 * r]);
+                float4* d = reinterpret_cast<float4*>(&S.o[buf][warp][row][16 * r]);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
                     d[y] = make_float4(o[b][2 * y][e], o[b][2 * y][e + 2], o[b][2 * y + 1][e], o[b][2 * y + 1][e + 2]);
@@ -306,8 +311,8 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
         const bool whole = I.part < 0;
         float* part = whole ? nullptr : partial_of<kRows4>(a, blockIdx.x, I.part == 0);
         for (int row = warp; row < rows; row += kWarps4) {
-            float wm = lane < kWarps4 ? S.m[lane][row] : kNoRef;
-            const float wl = lane < kWarps4 ? S.l[lane][row] : 0.f;
+            float wm = lane < kWarps4 ? S.m[buf][lane][row] : kNoRef;
+            const float wl = lane < kWarps4 ? S.l[buf][lane][row] : 0.f;
             const float M = redux_max(wm);
             wm = ex2_approx(wm - M);  // (of a warp that saw no key: 0, or 1 for 0 keys)
             const float L = warp_sum(wm * wl);
@@ -315,7 +320,7 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
 #pragma unroll
             for (int y = 0; y < kWarps4; ++y) {
                 const float f = __shfl_sync(0xffffffffu, wm, y);
-                const float4 v = *reinterpret_cast<const float4*>(&S.o[y][row][4 * lane]);
+                const float4 v = *reinterpret_cast<const float4*>(&S.o[buf][y][row][4 * lane]);
                 acc.x += v.x * f;
                 acc.y += v.y * f;
                 acc.z += v.z * f;
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(kThreads4, kCtas4) attention_few_q4_kernel(con
                 }
             }
         }
-        __syncthreads();
+        if (FewSmem4<N8>::kBufs == 1 || !whole) __syncthreads();
         if (whole) continue;
         if (threadIdx.x == 0) S.verdict = last_part(a, I);
         __syncthreads();
@@ -348,7 +353,8 @@ template <int N8>
 cudaError_t launch_few_q4(const AttnLaunch& L, AttnParams& p, cudaStream_t stream) {
     auto kern = attention_few_q4_kernel<N8>;
     static bool configured[kAttnMaxDevices] = {};
-    constexpr int bytes = static_cast<int>(sizeof(FewSmem4<N8>));
+    using SM = FewSmem4<N8>;
+    constexpr int bytes = static_cast<int>(sizeof(SM));
     static_assert(bytes <= 115712, "shared memory of two CTAs");
     const cudaError_t e = attn_configure(kern, bytes, configured);
     if (e != cudaSuccess) return e;
@@ -358,7 +364,7 @@ cudaError_t launch_few_q4(const AttnLaunch& L, AttnParams& p, cudaStream_t strea
     if (L.max_ctas > 0 && L.max_ctas < sms) grid = L.max_ctas;  // (two could go to an SM each)
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
     NvtxRange range("attention_few_q4_kernel");
-    kern<<<grid, kThreads4, bytes, stream>>>(p);
+    kern<<<grid, 32 * SM::kWarps4, bytes, stream>>>(p);
     return cudaGetLastError();
 }
 
