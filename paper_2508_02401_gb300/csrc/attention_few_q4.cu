@@ -73,11 +73,10 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         Walk w(p, S.run, p.tp, heads, S.scan);
         if (lane == 0) {
             new (walk) Walk(w);
-            if (walk->next(S.items[0])) walk->next(S.items[1]);
+            walk->next(S.items[0]);
         }
     }
     __syncthreads();
-    if (threadIdx.x == kThreads4 - 32 && S.items[0].part != kEndItem) walk->next(S.items[2]);  // (read after the next barrier)
 
     // A thread's place in a block of a page: K's and V's codes and scales.
     const int key = 4 * (r >> 1) + (r & 1);
@@ -131,6 +130,11 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         if (I.part == kEndItem) return;
         now = window(I, 0);
         if (steps_of(I) > 0) load(x, I, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
+        if (threadIdx.x == kThreads4 - 32) {  // beside the loads
+            walk->next(S.items[1]);
+            walk->next(S.items[2]);
+        }
+        __syncthreads();
     }
     for (int it = 0;; ++it) {
         const Item& I = S.items[it & 3];
