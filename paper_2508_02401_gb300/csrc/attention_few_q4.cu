@@ -96,31 +96,48 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
             page = table_page(a, I.seq, a.table + static_cast<size_t>(I.seq) * a.max_blocks, (I.t0 * kTileKeys + (warp + i * kWarps4) * 16) >> shift);
         return page;
     };
-    auto load = [&](Step& x, const Item& I, int i, int page) {
-        if (page >= a.num_pages) {  // (reported; the sequence's rows are undefined)
+    // Where a step's 16 rows begin in K's codes of a page (those of the scales at half the way of the rows before); null for a page
+    // that is out of range (reported; the sequence's rows are undefined).
+    struct Place {
+        const uint8_t* codes;
+        const uint8_t* scales;
+    };
+    auto place = [&](const Item& I, int i, int page) {
+        if (page >= a.num_pages) return Place{nullptr, nullptr};
+        const int row = (warp + i * kWarps4) * 16 & ((1 << shift) - 1);
+        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift) + row * 8;
+        return Place{b + row * 8, b};
+    };
+    auto load_k = [&](Step& x, const Place& b) {
+        if (b.codes) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                x.k[y] = __ldg(reinterpret_cast<const uint4*>(b.codes + at_k + y * 32));
+                x.ks[y] = __ldg(reinterpret_cast<const unsigned short*>(b.scales + at_ks + y * 16));
+            }
+        } else {
             x.k[0] = x.k[1] = make_uint4(0u, 0u, 0u, 0u);
+            x.ks[0] = x.ks[1] = 0u;
+        }
+    };
+    auto load_v = [&](Step& x, const Place& b) {
+        if (b.codes) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                x.v[y] = __ldg(reinterpret_cast<const uint2*>(b.codes + at_v + y * 16));
+                x.vs[y] = __ldg(reinterpret_cast<const unsigned short*>(b.scales + at_vs + y * 8));
+            }
+        } else {
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 x.v[y] = make_uint2(0u, 0u);
                 x.vs[y] = 0u;
             }
-            x.ks[0] = x.ks[1] = 0u;
-            return;
         }
-        // (a uniform base, and the thread's places in 32 bits)
-        const int row = (warp + i * kWarps4) * 16 & ((1 << shift) - 1);
-        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift) + row * 8;
-        const uint8_t* b2 = b + row * 8;
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            x.k[y] = __ldg(reinterpret_cast<const uint4*>(b2 + at_k + y * 32));
-            x.ks[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_ks + y * 16));
-        }
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            x.v[y] = __ldg(reinterpret_cast<const uint2*>(b2 + at_v + y * 16));
-            x.vs[y] = __ldg(reinterpret_cast<const unsigned short*>(b + at_vs + y * 8));
-        }
+    };
+    auto load = [&](Step& x, const Place& b) {
+        load_k(x, b);
+        load_v(x, b);
     };
 
     int now = 0;
@@ -129,7 +146,7 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         const Item& I = S.items[0];
         if (I.part == kEndItem) return;
         now = window(I, 0);
-        if (steps_of(I) > 0) load(x, I, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
+        if (steps_of(I) > 0) load(x, place(I, 0, uniform(__shfl_sync(0xffffffffu, now, 0))));
         if (threadIdx.x == kThreads4 - 32) {  // beside the loads
             walk->next(S.items[1]);
             walk->next(S.items[2]);
@@ -176,20 +193,28 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         }
         if (n == 0 && nj > 0) {
             now = ahead;
-            load(x, J, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
+            load(x, place(J, 0, uniform(__shfl_sync(0xffffffffu, now, 0))));
         }
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
-            Step cur = x;
+            // The next step's rows are loaded as soon as this one's are used, K's behind the logits and V's behind the output; with 16
+            // rows, where fewer warps hide a load, now.  (8 caches of 131072 tokens, 4 rows, 275 us, 293 with all of them now; 40 of
+            // 512 to 16384, 14 rows, 54 and 51.)
+            Step here;
+            if constexpr (N8 == 2) here = x;
+            Step& cur = N8 == 2 ? here : x;
+            Place next{nullptr, nullptr};
             if (i + 1 < n) {
                 if (((i + 1) & 31) == 0) {
                     now = ahead;
                     ahead = n > i + 33 ? window(I, i + 33) : nj > 0 ? window(J, 0) : 0;
                 }
-                load(x, I, i + 1, uniform(__shfl_sync(0xffffffffu, now, (i + 1) & 31)));
+                next = place(I, i + 1, uniform(__shfl_sync(0xffffffffu, now, (i + 1) & 31)));
+                if constexpr (N8 == 2) load(x, next);
             } else if (nj > 0) {
                 now = ahead;
-                load(x, J, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
+                next = place(J, 0, uniform(__shfl_sync(0xffffffffu, now, 0)));
+                if constexpr (N8 == 2) load(x, next);
             }
             const int k0 = I.t0 * kTileKeys + (warp + i * kWarps4) * 16;
             // ---- logits
@@ -214,6 +239,7 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
                     }
                 }
             }
+            if constexpr (N8 == 1) load_k(x, next);
             // ---- numerators
             if (k0 + 16 > I.pos0 + 1) {  // some row does not see some key
                 const int j = k0 + key;
@@ -272,7 +298,7 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
             {
                 const uint32_t c01 = __byte_perm(cur.vs[0], cur.vs[1], 0x5410), c23 = __byte_perm(cur.vs[2], cur.vs[3], 0x5410);
                 const uint32_t s01 = c01 & 0xfff0fff0u, s23 = c23 & 0xfff0fff0u;
-                const uint32_t z01 = (c01 & 0x000f000fu) | 0x43004300u, z23 = (c23 & 0x000f000fu) | 0x43004300u;
+                const uint32_t z01 = kv4_pair(c01), z23 = kv4_pair(c23);
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     const uint32_t v0 = w ? cur.v[0].y : cur.v[0].x, v1 = w ? cur.v[1].y : cur.v[1].x;
@@ -289,6 +315,7 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
                     }
                 }
             }
+            if constexpr (N8 == 1) load_v(x, next);
         }
         const int buf = it & (FewSmem4<N8>::kBufs - 1);
         // ---- the unit's (or this part's) result: the warps' outputs side by side, then a warp a row
