@@ -6,8 +6,22 @@
 //   K  (rows: keys)      thread (r, c) = (lane / 4, lane % 4): group c of keys 4 (r / 2) + r % 2 and 2 on, 16 bytes of each
 //   Q  (columns: rows)   row r, channels 32 c to 32 c + 31: 64 bytes
 //   V  (rows: channels)  channels 16 r to 16 r + 15 of keys 4 c to 4 c + 3, 8 bytes of each
-// A warp has a softmax of its own (reference, sums, output); the eight of a CTA are joined at a unit's end, the parts of a
-// unit by the CTA that finishes last.
+// A warp has a softmax of its own (reference, sums, output); the warps of a CTA are joined at a unit's end, the parts of a
+// unit by the CTA that finishes last.  No warp waits for another within a unit, and no thread for a copy.
+//
+// Bound by the instructions that make bf16 numbers of codes, not by memory (0.28 of a bf16 cache's bytes): a step of 16 keys
+// is some 415 instructions, 112 of them shifts and masks and 128 differences and products of two bf16 numbers, all of which issue
+// at half rate.  8 caches of 131072 tokens, one new token (4 rows a KV head, 1.21 GB): 274 us, 4.4 TB/s (a bf16 cache, 4.29 GB,
+// 623 us); the schedulers issue in 58 to 63% of the cycles, the rest is four warps' latencies.  With the differences, products
+// and masks left out (wrong results) the same loop took 241 us.  Legacy MMAs, since their operands come from registers, where the
+// codes are unpacked; of the tensor core's time 18% is used.  What else was built, us on those caches:
+//   tcgen05, keys on M: K unpacked into tensor memory, V into shared memory            425
+//   tcgen05 on the codes as 8-bit floats, numerators as pairs of those (too coarse)      339
+//   packed blocks by bulk copies into a ring of the CTA, scales behind the MMAs        305
+//   a ring of asynchronous copies for each warp                                        312
+//   8-bit-float MMAs for the logits                                                    334
+//   9 or 10 warps a CTA 327; one CTA of 16 warps 282 against 286, but 64 caches of 128 to 8192 74 against 50
+//   two steps a trip of the loop 288; the second next step asked into L2 306
 #include <new>
 #include <string.h>
 
@@ -30,7 +44,8 @@ struct Step {
     uint32_t ks[2], vs[4];  // scale words
 };
 
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -45,7 +60,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 // N8: blocks of 8 rows (1 or 2).
 template <int N8>
 struct FewSmem4 {
-    static constexpr int kWarps4 = N8 == 1 ? 8 : 6;  // (two CTAs of 168 registers a thread: 40 sequences, 14 rows each, 49 us, one CTA of 12 warps 57)
+    // 16 rows: 168 registers a thread, so six warps a CTA (40 sequences, 14 rows each, 49 us; one CTA of 12 warps 57).
+    static constexpr int kWarps4 = N8 == 1 ? 8 : 6;
     static constexpr int kBufs = N8 == 1 ? 2 : 1;  // of the warps' outputs (two: no barrier after they are read)
     float o[kBufs][kWarps4][8 * N8][kPitch4];
     float m[kBufs][kWarps4][8 * N8], l[kBufs][kWarps4][8 * N8];
@@ -93,11 +109,12 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         const int i = i0 + lane;
         int page = a.num_pages;
         if (i < steps_of(I))
-            page = table_page(a, I.seq, a.table + static_cast<size_t>(I.seq) * a.max_blocks, (I.t0 * kTileKeys + (warp + i * kWarps4) * 16) >> shift);
+            page = table_page(a, I.seq, a.table + static_cast<size_t>(I.seq) * a.max_blocks,
+                              (I.t0 * kTileKeys + (warp + i * kWarps4) * 16) >> shift);
         return page;
     };
-    // Where a step's 16 rows begin in K's codes of a page (those of the scales at half the way of the rows before); null for a page
-    // that is out of range (reported; the sequence's rows are undefined).
+    // Where a step's 16 rows begin in K's codes of a page, and in its scales (16 and 8 bytes a row before them); null for a
+    // page that is out of range (reported; the sequence's rows are undefined).
     struct Place {
         const uint8_t* codes;
         const uint8_t* scales;
@@ -105,7 +122,8 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
     auto place = [&](const Item& I, int i, int page) {
         if (page >= a.num_pages) return Place{nullptr, nullptr};
         const int row = (warp + i * kWarps4) * 16 & ((1 << shift) - 1);
-        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride + static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift) + row * 8;
+        const uint8_t* b = static_cast<const uint8_t*>(a.k) + page * a.page_stride +
+                           static_cast<long long>(I.g) * (2 * kKv4RowBytes << shift) + row * 8;
         return Place{b + row * 8, b};
     };
     auto load_k = [&](Step& x, const Place& b) {
@@ -304,8 +322,10 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
                     const uint32_t v0 = w ? cur.v[0].y : cur.v[0].x, v1 = w ? cur.v[1].y : cur.v[1].x;
                     const uint32_t v2 = w ? cur.v[2].y : cur.v[2].x, v3 = w ? cur.v[3].y : cur.v[3].x;
                     // even channels of two keys, odd channels
-                    const uint4 e01 = kv4_word(__byte_perm(v0, v1, 0x5410), s01, z01), d01 = kv4_word(__byte_perm(v0, v1, 0x7632), s01, z01);
-                    const uint4 e23 = kv4_word(__byte_perm(v2, v3, 0x5410), s23, z23), d23 = kv4_word(__byte_perm(v2, v3, 0x7632), s23, z23);
+                    const uint4 e01 = kv4_word(__byte_perm(v0, v1, 0x5410), s01, z01);
+                    const uint4 d01 = kv4_word(__byte_perm(v0, v1, 0x7632), s01, z01);
+                    const uint4 e23 = kv4_word(__byte_perm(v2, v3, 0x5410), s23, z23);
+                    const uint4 d23 = kv4_word(__byte_perm(v2, v3, 0x7632), s23, z23);
 #pragma unroll
                     for (int b = 0; b < N8; ++b) {
                         mma16816(o[b][4 * w], e01.x, d01.x, e23.x, d23.x, pb[b][0], pb[b][1]);
@@ -360,7 +380,8 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
             const int t = row / p.hp, h = row - t * p.hp;
             if (whole) {
                 const float inv = 1.f / L;
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + lane * 4;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) +
+                                     (static_cast<long long>(I.q_row + t) * a.Hq + I.head0 + h) * kHeadDim + lane * 4;
                 *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
                 if (lane == 0) write_lse<false>(a, I, t, h, M, L);
             } else {
@@ -409,11 +430,10 @@ cudaError_t launch_attention_few_q4(const AttnLaunch& L, int rows, cudaStream_t 
     p.hp = p.G;
     p.tp = (rows <= 8 ? 8 : 16) / p.G;
     p.nhb = 1;
-    p.unit_cost = 2;
+    p.unit_cost = 2;  // key tiles (64 caches of 128 to 8192: 45.7 us; 1: 51.4, 3: 47.2, 6: 52.4)
     p.min_run = 1;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;
-    p.wait_cycles = wait_limit_cycles();
     return rows <= 8 ? launch_few_q4<1>(L, p, stream) : launch_few_q4<2>(L, p, stream);
 }
 

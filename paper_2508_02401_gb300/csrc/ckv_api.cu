@@ -1715,9 +1715,9 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // with 2 each 69.4 / 110, which costs a chunk among as many single ones (64 and 64: 131 / 88) and most of all one
     // among idle sequences (256 tokens, 255 idle: 692 / 49).
     const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
-    // Over a cache of 4 bits, where the tile kernel unpacks a sequence's cache for every 256 rows, few / tiles: 64 sequences of
-    // 2000, 4 tokens each, 68 / 170, a chunk of 128 over 8000 among 64 single ones 130 / 128, a chunk of 512 among 256 465 / 441;
-    // 64 tokens and 64 idle sequences 79 / 45.
+    // Over a cache of 4 bits, where the tile kernel unpacks a sequence's cache for every 256 rows, few / tiles: 8 sequences
+    // of 8000, 4 rows 30 / 84, 8 rows 31 / 82, 12 rows 39 / 84, 16 rows 40 / 82; 64 of 2000, 4 tokens each, 70 / 170; a chunk of
+    // 128 over 8000 among 64 single tokens 137 / 128, of 512 among 256 492 / 441; 64 tokens and 63 idle sequences 74 / 45.
     const bool few = L.paged && rows <= 16 && (L.q4 || T <= 2 * S || (T - S + 1) * G <= 64);
     CUtensorMap mq, mk{}, mv{};  // (a cache of 4 bits has no maps)
     ckv_status st;

@@ -359,7 +359,7 @@ def test_refusals():
         with pytest.raises(ckv.CkvError):
             call(k=both[:20 * 256].view(20, 2, 128), k_out=both[256:21 * 256].view(20, 2, 128))
         with pytest.raises(ckv.CkvError, match="over one of its inputs"):
-            call(k_out=a.v.contiguous() if False else a.v)
+            call(k_out=a.v)
         with pytest.raises(ckv.CkvError, match="rotary_dim"):
             call(rotation=ckv.new_rotation(5000, rotary_dim=24))
     for bad in (torch.zeros((4, 2, 2, 16 * 72), dtype=torch.int8, device="cuda"), torch.zeros((4, 2, 2, 16 * 71), dtype=torch.uint8, device="cuda"),

@@ -7,7 +7,6 @@ import numpy as np
 import pytest
 import torch
 
-import oracle
 import paper_2508_02401_gb300 as ckv
 from tests import attention_ref as ref
 from tests import kv4_ref
