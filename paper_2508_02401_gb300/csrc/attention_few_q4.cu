@@ -21,7 +21,9 @@
 //   a ring of asynchronous copies for each warp                                        312
 //   8-bit-float MMAs for the logits                                                    334
 //   9 or 10 warps a CTA 327; one CTA of 16 warps 282 against 286, but 64 caches of 128 to 8192 74 against 50
-//   two steps a trip of the loop 288; the second next step asked into L2 306
+//   two steps a trip of the loop 288; a later step asked into L2, its rows 306, its pages by bulk prefetches 290
+//   s n in one fused operation, the zero points' part by MMAs of their own (fewer instructions, longer chains, and
+//   the small channels of a group with a large one cancel) 295
 #include <new>
 #include <string.h>
 
