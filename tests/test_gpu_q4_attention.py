@@ -210,6 +210,18 @@ def test_logits_of_any_size(new):
     c.check()
 
 
+@pytest.mark.parametrize("scale", [0.01, 0.4])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_a_given_scale(new, scale):
+    c = Paged4(config(12, 2, softmax_scale=scale), (3000, 260), (new, 1), 32, seed=36)
+    out, lse = c.run()
+    for s, (L, n) in enumerate(zip(c.lens, c.new)):
+        a = int(c.cu[s])
+        o, l, tol, tol_l = ref.rows(c.q[a:a + n], c.k[s], c.v[s], torch.arange(L - n, L), scale)
+        ref.assert_close(out[a:a + n], o, tol, f"out of sequence {s}")
+        ref.assert_close(lse[:, a:a + n], l, tol_l, f"lse of sequence {s}")
+
+
 def test_offset_cu_and_strided_q():
     """cu_new as a slice of a longer array (it need not begin at 0), q inside a fused projection."""
     c = Paged4(config(8, 2), (300, 40, 513), (1, 7, 33), 32, seed=8)
