@@ -8,10 +8,11 @@
 // Bound by memory: every row is read once and written once or twice.  A half-warp takes four rows of one token, 16 bytes a
 // lane and row, with the token's angles in registers: loaded once for four rows they cost half of what a row does.
 // 40001 kept rows into 4 bits, no rotation (370 MB): 66 us, 5.6 TB/s.  20525 tokens with queries (28 / 4 heads, keys kept too,
-// 407 MB): 80 us, 5.1 TB/s; 8192 of 32 / 8 heads 45 us, 4.9; 7097 into 4 bits 33 us, 4.2, where the rotation and the
-// codes keep the schedulers at work two cycles in three.  Four CTAs an SM (64 registers): with 3 / 4 / 5 the second took 90.8 /
-// 80.2 / 81.5 us, the third 49.9 / 45.2 / 42.5, the fourth 35.9 / 33.1 / 34.8.  A decode step's append is a launch and
-// one chain of loads (64 tokens: 2.8 us on the GPU, 3.6 into 4 bits).
+// 407 MB): 77 us, 5.3 TB/s; 8192 of 32 / 8 heads 43 us, 5.1; 7097 into 4 bits 33 us, 4.2, where the rotation and the
+// codes keep the schedulers at work two cycles in three.  36 warps an SM (56 registers): with 24 / 28 / 32 / 36 / 40 the second
+// took 90.8 / 83.6 / 79.5 / 77.0 / 80.0 us, the third 49.9 / 46.7 / 45.0 / 43.1 / 42.3, the fourth 35.9 / 34.2 / 33.1 / 32.8 /
+// 33.8; two rows a half-warp 97, 48 and 39, eight 79, 43 and 37; the warps of a token side by side, for its angles, 78, 42 and 33.
+// A decode step's append is a launch and one chain of loads (64 tokens: 2.8 us on the GPU, 3.6 into 4 bits).
 #include <float.h>
 
 #include "ckv_device.cuh"
@@ -21,7 +22,7 @@
 namespace ckv {
 namespace {
 
-constexpr int kAppThreads = 256;
+constexpr int kAppThreads = 128, kAppCtas = 9;
 constexpr int kAppToks = kAppThreads / 16;  // tokens of a CTA
 constexpr int kAppQ = 4, kAppKv = 2;        // query heads, KV heads (a row of K and one of V each) of a half-warp
 constexpr int kAppRows = 4;
@@ -121,7 +122,7 @@ __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
 }
 
 template <bool Q4, int ROT>
-__global__ void __launch_bounds__(kAppThreads, 4) cache_append_kernel(const __grid_constant__ AppendLaunch p) {
+__global__ void __launch_bounds__(kAppThreads, kAppCtas) cache_append_kernel(const __grid_constant__ AppendLaunch p) {
     const int c = threadIdx.x & 15;
     const int nq = p.q ? (p.Hq + kAppQ - 1) / kAppQ : 0, chunks = nq + (p.Hkv + kAppKv - 1) / kAppKv;
     const int block = blockIdx.x / chunks, ch = blockIdx.x - block * chunks;
