@@ -11,9 +11,9 @@
 //
 // Bound by the instructions that make bf16 numbers of codes, not by memory (0.28 of a bf16 cache's bytes): a step of 16 keys
 // is some 415 instructions, 112 of them shifts and masks and 128 differences and products of two bf16 numbers, all of which issue
-// at half rate.  8 caches of 131072 tokens, one new token (4 rows a KV head, 1.21 GB): 274 us, 4.4 TB/s (a bf16 cache, 4.29 GB,
+// at half rate.  8 caches of 131072 tokens, one new token (4 rows a KV head, 1.21 GB): 269 us, 4.5 TB/s (a bf16 cache, 4.29 GB,
 // 623 us); the schedulers issue in 58 to 63% of the cycles, the rest is four warps' latencies.  With the differences, products
-// and masks left out (wrong results) the same loop took 241 us.  Legacy MMAs, since their operands come from registers, where the
+// and masks left out (wrong results) a form of the loop took 241 us.  Legacy MMAs, since their operands come from registers, where the
 // codes are unpacked; of the tensor core's time 18% is used.  What else was built, us on those caches:
 //   tcgen05, keys on M: K unpacked into tensor memory, V into shared memory            425
 //   tcgen05 on the codes as 8-bit floats, numerators as pairs of those (too coarse)      339
