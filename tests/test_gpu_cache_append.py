@@ -288,6 +288,35 @@ def test_offsets_beyond_32_bits(q4):
 
 
 @pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("layer", [0, 2])
+def test_pages_of_layers_side_by_side(q4, layer):
+    """One buffer with three layers' pages between each other: the others' bytes stay."""
+    a = Append(70, page=32, q4=q4, seed=18, queries=False)
+    shape = (a.num_pages, 3, a.hkv, 2, 32 * 72) if q4 else (a.num_pages, 3, 2, 32, a.hkv, 128)
+    both = torch.full(shape, 7, dtype=torch.uint8 if q4 else BF, device="cuda")
+    mine = both[:, layer]
+    if q4:
+        ckv.ckv_cache_append_q4(a.cfg, ckv.PagedCacheQ4(mine, 32), a.k, a.v, a.slots, a.ws, rotation=a.rot, positions=a.positions)
+    else:
+        ckv.ckv_cache_append(a.cfg, ckv.PagedCache(mine[:, 0], mine[:, 1]), a.k, a.v, a.slots, a.rot, a.positions, a.ws)
+    assert ckv.ckv_read_device_status(a.ws) == (0, 0)
+    want, k = torch.full_like(both, 7), kv4_ref.rotate(a.k, a.rot.cos_sin, a.positions)
+    for i, x in enumerate((k, a.v)):
+        if q4:
+            kv4_ref.put(want[:, layer], 32, a.slots, x, i)
+        else:
+            want[a.slots.long() // 32, layer, i, a.slots.long() % 32] = x
+    same(both, want)
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_no_tokens(q4):
+    a = Append(0, q4=q4, seed=19)
+    pages, _ = a.run(outs=False)
+    assert bool((pages == (0xA5 if q4 else 7)).all())
+
+
+@pytest.mark.parametrize("q4", [False, True])
 def test_captured_and_replayed(q4):
     """One captured call over device positions and slots: each replay sees those of its time; on another stream too."""
     a = Append(33, q4=q4, seed=16)

@@ -222,6 +222,17 @@ def test_a_given_scale(new, scale):
         ref.assert_close(lse[:, a:a + n], l, tol_l, f"lse of sequence {s}")
 
 
+def test_no_tokens():
+    """Sequences without query rows: nothing is written, whatever their lengths."""
+    c = Paged4(config(8, 2), (300, 0, 40), (0, 0, 0), 16, seed=37, pad=2)
+    out, lse = c.run()
+    assert bool((out == 7).all()) and bool((lse == 7).all())
+    none = torch.zeros((0, 8, 128), dtype=torch.bfloat16, device="cuda")
+    ws = ckv.new_attention_workspace(c.cfg)
+    ckv.ckv_paged_attention_q4(c.cfg, ckv.PagedCacheQ4(c.pages, 16), dev(c.table), dev(c.lens), dev(c.cu), none, torch.empty_like(none), ws)
+    assert ckv.ckv_read_device_status(ws) == (0, 0)
+
+
 def test_offset_cu_and_strided_q():
     """cu_new as a slice of a longer array (it need not begin at 0), q inside a fused projection."""
     c = Paged4(config(8, 2), (300, 40, 513), (1, 7, 33), 32, seed=8)
