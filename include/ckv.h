@@ -573,8 +573,8 @@ CKV_API ckv_status ckv_paged_attention(const ckv_config* cfg, const ckv_paged_ca
 
 /* ckv_paged_attention over a cache of 4 bits: the same call, lengths, outputs and status codes.  The values of the cache
  * enter both products as they are (bf16 numbers).  Here up to 16 (token, query head) rows per KV head a sequence, by num_tokens
- * against num_seqs, are taken for few tokens, whatever their spread: a long chunk among single tokens or idle sequences is slower
- * in such a call than by itself. */
+ * against num_seqs (32 in calls with few tokens), are taken for few tokens, whatever their spread: a long chunk among single
+ * tokens or idle sequences is slower in such a call than by itself. */
 CKV_API ckv_status ckv_paged_attention_q4(const ckv_config* cfg, const ckv_paged_cache_q4* cache,
                                           int32_t num_seqs, int32_t num_tokens, const int32_t* block_table,
                                           int32_t max_blocks, const int32_t* cache_lens, const int32_t* cu_new,

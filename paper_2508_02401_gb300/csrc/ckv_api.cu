@@ -1718,7 +1718,12 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // Over a cache of 4 bits, where the tile kernel unpacks a sequence's cache for every 256 rows, few / tiles: 8 sequences
     // of 8000, 4 rows 30 / 84, 8 rows 31 / 82, 12 rows 39 / 84, 16 rows 40 / 82; 64 of 2000, 4 tokens each, 70 / 170; a chunk of
     // 128 over 8000 among 64 single tokens 137 / 128, of 512 among 256 492 / 441; 64 tokens and 63 idle sequences 74 / 45.
-    const bool few = L.paged && rows <= 16 && (L.q4 || T <= 2 * S || (T - S + 1) * G <= 64);
+    // Up to 32 rows, which the few-rows kernel takes in two passes, where no sequence can have over 256: 8 of 8000 with 8 tokens
+    // each 62 / 82, one 25 / 39, of 131072 109 / 151 (with 12 155 / 158), 2 of 300 14.7 / 16.7; a chunk of 57 among 7 single
+    // tokens 79 / 89, but over 60000 with short ones beside it 333 / 117.  64 of 2000 with 8 tokens each, 121 / 170, stay with the
+    // tiles for the chunk of 449 that could be among them, 362 / 172.
+    const bool few = L.paged && (L.q4 ? rows <= 16 || (rows <= 32 && G <= 16 && (T - S + 1) * G <= 256)
+                                      : rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64));
     CUtensorMap mq, mk{}, mv{};  // (a cache of 4 bits has no maps)
     ckv_status st;
     if (!few) {

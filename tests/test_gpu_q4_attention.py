@@ -91,7 +91,7 @@ def test_unusual_groups(hq, hkv, new):
     Paged4(config(hq, hkv), (700, 131, 40), (new, new, new), 16, seed=5).check(pad=3)
 
 
-@pytest.mark.parametrize("new", [1, 2, 3, 4, 5, 70])
+@pytest.mark.parametrize("new", [1, 2, 3, 4, 5, 8, 9, 70])
 @pytest.mark.parametrize("max_ctas", [0, 5])
 def test_long_caches_are_cut_and_joined(new, max_ctas):
     Paged4(config(8, 2, max_ctas=max_ctas), (20011, 77, 9000), (new, new, 1), 64, seed=6).check()

@@ -16,7 +16,7 @@ def arguments(c):
     return [torch.as_tensor(x, dtype=torch.int32, device="cuda") for x in (c.table, c.lens, c.cu)]
 
 
-@pytest.mark.parametrize("new", [5, 8, 70])
+@pytest.mark.parametrize("new", [9, 20, 70])
 def test_chunks(one_microsecond, new):  # noqa: F811
     c = Paged4(config(), (3000, 700, 90), (new,) * 3, 32, seed=21)
     ws, cache, out = ckv.new_attention_workspace(c.cfg), ckv.PagedCacheQ4(c.pages, 32), torch.zeros_like(c.q)
@@ -34,7 +34,7 @@ def test_chunks(one_microsecond, new):  # noqa: F811
         ref.assert_close(out[a:a + n], o, tol, f"sequence {s}")
 
 
-@pytest.mark.parametrize("new", [1, 2, 4])
+@pytest.mark.parametrize("new", [1, 2, 4, 8])
 def test_few_rows_wait_for_nothing(one_microsecond, new):  # noqa: F811
     Paged4(config(), (3000, 700, 90), (new,) * 3, 32, seed=21).check()
 
