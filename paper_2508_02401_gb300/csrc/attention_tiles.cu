@@ -46,7 +46,8 @@ struct TilesSmem {
                          kPackedFree = kPackedFull + kPacked, kNumBars = kPackedFree + kPacked;
     static constexpr int kScan = kBars + 8 * kNumBars;
     static constexpr int kMisc = kScan + kScanBytes;  // TMEM base, abort, verdict
-    static constexpr int kBytes = kMisc + 16;
+    static constexpr int kLoaded = kMisc + 16;        // of the packed tiles: which pages were loaded
+    static constexpr int kBytes = kLoaded + 4 * kPacked;
     static_assert(kBytes <= 232448, "shared memory");
 };
 
@@ -303,6 +304,7 @@ __global__ void __launch_bounds__(TilesSmem<SRC>::kThreads, 1) attention_tiles_k
         // ---------------------------------------------------------------- packed tiles into bf16 tiles, a key a thread
         setmaxnreg_dec<64>();
         uint8_t* packed = sm + SM::kPackedRing;
+        const uint32_t* loaded = reinterpret_cast<const uint32_t*>(sm + SM::kLoaded);
         const int key = threadIdx.x & 127;
         uint32_t in = 0, in_phase = 0, to = 0, to_phase = 1;
         bool ok = true, live = true;  // live (a lane's own): none of its waits for a packed tile gave up
@@ -319,6 +321,7 @@ __global__ void __launch_bounds__(TilesSmem<SRC>::kThreads, 1) attention_tiles_k
                 __syncwarp();
                 Kv4Row r = kv4_row(packed + in * kPackedTile + static_cast<uint32_t>(key >> p.page_shift) * (kKv4RowBytes << p.page_shift),
                                    p.page_shift, key & ((1 << p.page_shift) - 1));
+                const uint32_t pages = loaded[in];
                 // (the reads before the copy that goes over them: without this fence the next copy overtook some)
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -327,8 +330,9 @@ __global__ void __launch_bounds__(TilesSmem<SRC>::kThreads, 1) attention_tiles_k
                     in = 0;
                     in_phase ^= 1;
                 }
-                // Rows behind the sequence's end hold anything, and while their numerators are 0, 0 * NaN is not.
-                if (key >= keys - (u >> 1) * kTileKeys) r.scales = make_uint2(0u, 0u);
+                // Rows behind the sequence's end hold anything, and while their numerators are 0, 0 * NaN is not.  Rows of a page that
+                // was not loaded are what an earlier tile left.
+                if (key >= keys - (u >> 1) * kTileKeys || !(pages >> (key >> p.page_shift) & 1u)) r.scales = make_uint2(0u, 0u);
                 tile_wait(&freed[to], to_phase, abort, lim, a.status);
                 __syncwarp();
                 unpack_row(r, ring + to * kTileBytes, key);
@@ -354,7 +358,8 @@ __global__ void __launch_bounds__(TilesSmem<SRC>::kThreads, 1) attention_tiles_k
             Walk walk(p, run, tq, heads, scan);
             auto tiles = [&] {
                 if constexpr (kQ4)
-                    return PackedLoader<SM::kPacked>{p, sm + SM::kPackedRing, bars + SM::kPackedFull, bars + SM::kPackedFree, abort, lim};
+                    return PackedLoader<SM::kPacked>{p, sm + SM::kPackedRing, bars + SM::kPackedFull, bars + SM::kPackedFree,
+                                                     reinterpret_cast<uint32_t*>(sm + SM::kLoaded), abort, lim};
                 else
                     return TileLoader<SRC == kPaged, kRingT>{p, ring, full, freed, abort, lim};
             }();

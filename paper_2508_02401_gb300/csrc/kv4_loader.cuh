@@ -19,13 +19,14 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 
 // One warp loads an item's packed tiles into the ring: K0 V0 K1 V1 ..., a page a lane (its block of K or V is one copy:
 // a multiple of 1152 bytes at such an offset, so the 16-byte rule of copies holds for any page size).  A page that is out of
-// range is not loaded.
+// range is not loaded: `loaded` has a bit a page of each slot's tile, for the unpacking warps, to which the others' rows are zeros.
 template <int RING>
 struct PackedLoader {
     const AttnParams& p;
     uint8_t* ring;
     uint64_t* full;
     uint64_t* freed;
+    uint32_t* loaded;
     volatile int* abort;
     long long lim;
     uint32_t slot = 0, phase = 1, use = 0;
@@ -36,8 +37,11 @@ struct PackedLoader {
         const int lane = threadIdx.x & 31;
         const uint32_t bytes = kKv4RowBytes << p.page_shift;
         const bool mine = lane >= first && lane < first + (kTileKeys >> p.page_shift) && page < a.num_pages;
-        const uint32_t pages = __popc(__ballot_sync(0xffffffffu, mine));
-        if (lane == 0) mbar_arrive_expect_tx(&full[slot], pages * bytes);
+        const uint32_t pages = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) {
+            loaded[slot] = pages >> first;  // (published by the arrival)
+            mbar_arrive_expect_tx(&full[slot], __popc(pages) * bytes);
+        }
         __syncwarp();
         if (mine)
             bulk_load(ring + slot * kPackedTile + (lane - first) * bytes,

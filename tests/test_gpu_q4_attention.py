@@ -371,6 +371,23 @@ def test_bad_lengths_and_pages_are_reported(what, new):
         ref.assert_close(lse[:, a:b], l, tol_l, f"lse of sequence {s}")
 
 
+@pytest.mark.parametrize("hq,hkv,new", [(8, 2, 1), (8, 2, 3), (8, 2, 60), (28, 4, 300)])
+@pytest.mark.parametrize("max_ctas", [0, 1])
+@pytest.mark.parametrize("page", [16, 128])
+def test_a_bad_page_reads_as_zeros(hq, hkv, new, max_ctas, page):
+    """Bit for bit what a page of zero bytes gives, whatever was loaded before: the first and other sequences' rows are none of it."""
+    c = Paged4(config(hq, hkv, max_ctas=max_ctas), (2900, 1300, 700), (new, new, 1), page, seed=38)
+    c.pages = torch.cat([c.pages, torch.zeros_like(c.pages[:1])])
+    last = c.pages.shape[0] - 1
+    blocks = [0, 2, 5, 1300 // page] if page == 16 else [1, 4, 1300 // page]
+    c.table[1, blocks] = last
+    want = c.run()
+    for bad in (last + 1, -1, 2 ** 31 - 1):
+        c.table[1, blocks] = bad
+        got = c.run(status=(3, 0))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_refusals():
     c = Paged4(config(8, 2), (300, 200), (1, 1), 32, seed=15)
     cfg, cache, ws = c.cfg, ckv.PagedCacheQ4(c.pages, 32), ckv.new_attention_workspace(c.cfg)
