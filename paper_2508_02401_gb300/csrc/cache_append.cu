@@ -7,12 +7,13 @@
 //
 // Bound by memory: every row is read once and written once or twice.  A half-warp takes four rows of one token, 16 bytes a
 // lane and row, with the token's angles in registers: loaded once for four rows they cost half of what a row does.
-// 40001 kept rows into 4 bits, no rotation (370 MB): 66 us, 5.6 TB/s.  20525 tokens with queries (28 / 4 heads, keys kept too,
-// 407 MB): 77 us, 5.3 TB/s; 8192 of 32 / 8 heads 43 us, 5.1; 7097 into 4 bits 33 us, 4.2, where the rotation and the
-// codes keep the schedulers at work two cycles in three.  36 warps an SM (56 registers): with 24 / 28 / 32 / 36 / 40 the second
-// took 90.8 / 83.6 / 79.5 / 77.0 / 80.0 us, the third 49.9 / 46.7 / 45.0 / 43.1 / 42.3, the fourth 35.9 / 34.2 / 33.1 / 32.8 /
+// 40001 kept rows into 4 bits, no rotation (370 MB): 67 us, 5.5 TB/s.  20525 tokens with queries (28 / 4 heads, keys kept too,
+// 407 MB): 74.5 us, 5.5 TB/s; 8192 of 32 / 8 heads 42.5 us, 5.2; 7097 into 4 bits 32 us, 4.3, where the rotation and the
+// codes keep the schedulers at work.  36 warps an SM (56 registers, some spilled).  That, the rows and their order were measured with the
+// rare sums still inlined (the present form was 77.0, 43.1 and 32.8 us then): with 24 / 28 / 32 / 40 warps the second
+// took 90.8 / 83.6 / 79.5 / 80.0 us, the third 49.9 / 46.7 / 45.0 / 42.3, the fourth 35.9 / 34.2 / 33.1 /
 // 33.8; two rows a half-warp 97, 48 and 39, eight 79, 43 and 37; the warps of a token side by side, for its angles, 78, 42 and 33.
-// A decode step's append is a launch and one chain of loads (64 tokens: 2.8 us on the GPU, 3.6 into 4 bits).
+// A decode step's append is a launch and one chain of loads (64 tokens: 2.9 us on the GPU, 3.8 into 4 bits).
 #include <float.h>
 
 #include "ckv_device.cuh"
@@ -71,18 +72,43 @@ __device__ __forceinline__ void load_angles(const AppendLaunch& p, int pos, int 
     }
 }
 
-// a c + b s to the last bit of 32: the products' and the sum's rounding errors (exact by fused operations and the known
-// error of a sum of two) are added at the end.
-__device__ __forceinline__ float turn_exact(float a, float c, float b, float s) {
+// a c + b s, rounded to 32 bits.  In 64 bits the products are exact, and a sum rounded to odd (where bits are lost, the neighbour
+// whose last bit is 1) rounds to 32 bits as the exact one does.
+__device__ __forceinline__ float turn_wide(float a, float c, float b, float s) {
+    const double p = static_cast<double>(a) * c, q = static_cast<double>(b) * s, r = p + q, t = r - p, e = (p - (r - t)) + (q - t);
+    long long bits = __double_as_longlong(r);
+    if ((e > 0.0 || e < 0.0) && !(bits & 1)) bits += (e > 0.0) == (r > 0.0) ? 1 : -1;
+    return __double2float_rn(__longlong_as_double(bits));
+}
+
+// Bounds of the same: the products' and the sum's rounding errors (exact by fused operations and the known error of a sum
+// of two, but for 2^-149 where a product is below what fp32 holds to 24 bits) go to the sum, with their own roundings to either side.
+__device__ __forceinline__ void turn_bounds(float a, float c, float b, float s, float& lo, float& hi) {
     // (intrinsics: the compiler would fuse a product with a sum)
-    const float p = __fmul_rn(a, c), q = __fmul_rn(b, s), pe = fmaf(a, c, -p), qe = fmaf(b, s, -q);
+    const float p = __fmul_rn(a, c), q = __fmul_rn(b, s), u = __fadd_rn(fmaf(a, c, -p), fmaf(b, s, -q));
     const float r = __fadd_rn(p, q), t = __fadd_rn(r, -p), e = __fadd_rn(__fadd_rn(p, -__fadd_rn(r, -t)), __fadd_rn(q, -t));
-    return fabsf(r) <= FLT_MAX ? __fadd_rn(r, __fadd_rn(e, __fadd_rn(pe, qe))) : r;
+    const float v = __fadd_rn(e, u), d = fmaf(__fadd_rn(fabsf(u), fabsf(v)), 0x1p-22f, 0x1p-140f);
+    lo = __fadd_rn(r, __fadd_rn(v, -d));
+    hi = __fadd_rn(r, __fadd_rn(v, d));
+    if (!(hi - lo <= FLT_MAX)) lo = 1.f, hi = 0.f;  // (beyond fp32 on the way: bounds that differ)
+    if (a == 0.f && b == 0.f) lo = hi = r;          // (the bounds are -0 and 0)
+}
+
+// Two channels (x: their own values, y: the others of their pairs), where the fp32 results do not decide.  A function of its own:
+// inlined, with the sum in 64 bits or without, it costs the loops around it registers (20525 tokens 89 and 105 us, 74.6 so).
+__device__ __noinline__ uint32_t turn_pair(uint32_t x, uint32_t y, float c0, float s0, float c1, float s1) {
+    const float x0 = bf16_lo(x), x1 = bf16_hi(x), y0 = bf16_lo(y), y1 = bf16_hi(y);
+    float l[2], h[2];
+    turn_bounds(x0, c0, y0, s0, l[0], h[0]);
+    turn_bounds(x1, c1, y1, s1, l[1], h[1]);
+    const uint32_t lo = pack_bf16x2(l[0], l[1]);
+    if (lo == pack_bf16x2(h[0], h[1])) return lo;
+    return pack_bf16x2(turn_wide(x0, c0, y0, s0), turn_wide(x1, c1, y1, s1));
 }
 
 // A lane's 8 channels of a row, rotated (a whole half-warp).  The fp32 result r = a c + q, q = b s, is off by 2^-24 (|q| + |r|)
-// at most; where all numbers so near round to one bf16 number, that is the result (roundings keep the order of
-// numbers), otherwise (one pair in 2000) the sum is taken exactly.
+// at most, or by 2^-149 among the smallest numbers; where all numbers so near round to one bf16 number, that is the result (roundings
+// keep the order of numbers).  Otherwise (one pair in 2000) closer bounds decide, and where those differ too the sum in 64 bits.
 template <int ROT>
 __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
     const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
@@ -103,7 +129,7 @@ __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
         for (int e = 0; e < 2; ++e) {
             const float xf = e ? bf16_hi(x[i]) : bf16_lo(x[i]), yf = e ? bf16_hi(y[i]) : bf16_lo(y[i]);
             const float q = yf * A.s[2 * i + e], r = fmaf(xf, A.c[2 * i + e], q);
-            const float w = fabsf(q) + fabsf(r);
+            const float w = fabsf(q) + (fabsf(r) + 0x1p-124f);
             l[e] = fmaf(w, -0x1.00001p-24f, r);
             h[e] = fmaf(w, 0x1.00001p-24f, r);
         }
@@ -114,9 +140,7 @@ __device__ __forceinline__ uint4 rotate8(const uint4& x4, const Angles& A) {
     if (differ) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (lo[i] != hi[i])
-                lo[i] = pack_bf16x2(turn_exact(bf16_lo(x[i]), A.c[2 * i], bf16_lo(y[i]), A.s[2 * i]),
-                                    turn_exact(bf16_hi(x[i]), A.c[2 * i + 1], bf16_hi(y[i]), A.s[2 * i + 1]));
+            if (lo[i] != hi[i]) lo[i] = turn_pair(x[i], y[i], A.c[2 * i], A.s[2 * i], A.c[2 * i + 1], A.s[2 * i + 1]);
     }
     return make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }

@@ -181,6 +181,53 @@ def test_sums_that_cancel(q4):
     a.check()
 
 
+@pytest.mark.parametrize("q4", [False, True])
+def test_sums_next_to_a_tie(q4):
+    """c - b s with c a tie of bf16 and b s = +-2^-24 (1 + 127 / 2^31): by 2^-48 past what would still round to the tie in 32 bits.
+    From 1 + 2^-8 the sum above goes up, from 1 + 3 2^-8 (whose even neighbour is the upper one) the sum below goes down."""
+    a = Append(64, hq=4, hkv=2, q4=q4, seed=20)
+    a.rot.cos_sin[:, :64] = 1 + 2.0 ** -8 * torch.where(torch.arange(64, device="cuda") % 4 < 2, 1.0, 3.0)
+    a.rot.cos_sin[:, 64:] = 8421505 * 2.0 ** -48  # 255 * 8421505 = 2^31 + 127
+    b = 255 / 128 * torch.where(torch.arange(64, device="cuda") % 2 == 0, 1.0, -1.0)
+    for x in (a.q, a.k):
+        x[..., :64], x[..., 64:] = 1.0, b
+        x[::2] = x[::2].roll(64, -1)
+    a.check()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("low,high", [(-110, -90), (-130, -110), (-140, -125)])
+def test_tiny_rows(low, high, interleaved):
+    """Products and sums that fp32 has as subnormal numbers, results that bf16 has as such."""
+    a = Append(6000, hq=8, hkv=4, seed=21, interleaved=interleaved)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    for x in (a.q, a.k):
+        x.copy_((x.double() * torch.exp2(torch.randint(low, high, (*x.shape[:2], 1), generator=g, device="cuda").double())).to(BF))
+    a.check()
+
+
+def test_rows_with_zeros():
+    """Rows, words and single pairs of zeros."""
+    a = Append(200, hq=4, hkv=2, seed=24)
+    for x in (a.q, a.k):
+        x[::4] = 0
+        x[1::4, :, 6:60:2] = 0
+        x[1::4, :, 70:124:2] = 0
+        x[2::4, :, :64] = 0
+    a.check()
+
+
+def test_sums_beyond_the_products():
+    """Products that fp32 does not have, their sum within it, and sums beyond it."""
+    a = Append(40, hq=4, hkv=2, seed=23)
+    a.rot.cos_sin[:, :64], a.rot.cos_sin[:, 64:] = 1.75, 1.5
+    for x in (a.q, a.k):
+        x[..., :64], x[..., 64:] = 3e38, 3.2e38
+        x[::3, :, 64:] = 1.0
+        x[1::3] = -x[1::3]
+    a.check()
+
+
 @pytest.mark.parametrize("kind", ["constant", "zero", "positive", "negative", "outlier", "ties", "tiny", "huge", "signs", "edge"])
 def test_groups(kind):
     a = Append(500, q4=True, rd=0, queries=False, seed=10)
