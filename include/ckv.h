@@ -525,12 +525,12 @@ CKV_API ckv_status ckv_cache_append(const ckv_config* cfg, const ckv_paged_cache
  * (ckv_block_tables).  Page p begins at byte p * page_stride (0 = packed; a multiple of 16) and holds, per KV head,
  * K's block and then V's, each of page_size * 72 bytes: codes [4 groups][page_size][16 bytes], scales
  * [page_size][4 groups][2 bytes].
- *   A group is 32 channels x of a row.  With range = max(x, 0) - min(x, 0): its scale s is the least number of 4
- *   significant bits, 2^-100 at least, with 15 s >= range; its zero point z = round(-min(x, 0) / s); its codes
- *   n = clamp(round(x / s) + z, 0, 15), ties to even.  A value is s (n - z), within s / 2 of x, and a bf16 number.
+ *   A group is 32 channels x of a row.  With range = max(x, 0) - min(x, 0), rounded to fp32 (to nearest, ties to
+ *   even): its scale s is the least number of 4 significant bits, 2^-100 at least, with 15 s >= range; its zero point
+ *   z = round(-min(x, 0) / s); its codes n = clamp(round(x / s) + z, 0, 15), ties to even.  A value is s (n - z), within s / 2 of x, and a bf16 number.
  *   The 16 bytes of codes are four 32-bit words of 8 channels, channel c of a word in nibble c / 2 + 4 (c % 2) (bits 4 i
  *   to 4 i + 3); the scale's 16 bits are the bf16 pattern of s, whose low nibble is 0, with z there.
- *   A group with a NaN or an infinity has a NaN for s: all its values are NaN.  Values are below 1e38 in magnitude.
+ *   A group with a NaN, an infinity or a range beyond fp32 has a NaN for s: all its values are NaN.  Values are below 1e38 in magnitude.
  * Rows of a page behind a sequence's end are never used, so pages need no clearing. */
 typedef struct ckv_paged_cache_q4 {
     void* pages;          /* 16-byte aligned */

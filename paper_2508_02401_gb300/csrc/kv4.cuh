@@ -1,7 +1,9 @@
 // A row of 128 values in 4 bits: four groups of 32 channels, each with a scale s of 4 significant bits and a zero point z.
-//   wide = max(x, 0) - min(x, 0);  s = the least such number, 2^-100 at least, with 15 s >= wide
+//   wide = max(x, 0) - min(x, 0), rounded to fp32;  s = the least such number, 2^-100 at least, with 15 s >= wide
 //   z = round(-min(x, 0) / s),  n = clamp(round(x / s) + z, 0, 15)  (ties to even);  the value is s (n - z)
-// |value - x| <= s / 2: max / s - min / s <= 15, so a code is clamped only where two ties were both rounded up.  n - z
+// |value - x| <= s / 2: max / s - min / s <= 15, so a code is clamped only where two ties were both rounded up.  (The
+// rounding of the range changes nothing of it: where it does round, the smaller of max and -min is below 2^-15 of the range, its
+// codes are those of 0, and the larger is 15 s at most.)  n - z
 // has 4 bits and a sign, s 4 significant bits, so the value is a bf16 number: nothing that reads the cache rounds it.
 // A group with a NaN, an infinity or a range beyond fp32 has s = NaN: every value of it is NaN.
 //

@@ -11,6 +11,7 @@ import paper_2508_02401_gb300 as ckv
 from tests import kv4_ref
 from tests.gpu_util import Guarded
 from tests.test_gpu_prefill_attention import config, normal
+from tests.test_kv4_ref_cpu import far_apart
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -260,6 +261,12 @@ def test_groups(kind):
     x, h = a.k.double(), out["k_out"].double()
     _, s, _ = kv4_ref.quantise(a.k)
     assert bool(((h - x).abs() <= s.repeat_interleave(32, -1) / 2).all())
+
+
+def test_groups_whose_range_is_rounded():
+    a = Append(64, hkv=1, hq=1, q4=True, rd=0, queries=False, seed=25)
+    a.k, a.v = far_apart().cuda()[:, None], -far_apart().cuda()[:, None]
+    a.check()
 
 
 def test_values_that_are_not_finite():

@@ -49,6 +49,40 @@ def test_against_fractions(kind):
     assert torch.equal(held.to(torch.bfloat16).double(), held)  # a bf16 number
 
 
+def far_apart():
+    """Groups whose largest and smallest values are so far apart that fp32 rounds their difference: to 15 scales, where the exact one is
+    above (or below) them, and to others."""
+    x = torch.zeros(64, 128)
+    for i in range(64):
+        top = 15.0 * (1 + i % 8 / 8) * 2.0 ** (i % 5 - 2)
+        for j in range(4):
+            sign = 1 if (i + j) % 2 else -1
+            x[i, 32 * j + i % 32] = sign * top
+            x[i, 32 * j + (i + 7) % 32] = -sign * top * 2.0 ** -(17 + 3 * j + i // 16)
+            x[i, 32 * j + (i + 9) % 32] = sign * top * 0.5
+    return x.to(torch.bfloat16)
+
+
+def test_the_range_is_rounded():
+    x = far_apart()
+    codes, s, z = kv4_ref.quantise(x)
+    rounded = 0
+    scales = [Fraction(n, 8) * Fraction(2) ** e for e in range(-8, 8) for n in range(8, 16)]
+    for i in range(len(x)):
+        for j in range(4):
+            g = x[i, 32 * j:32 * j + 32]
+            wide = Fraction(float(g.max().float() - g.min().float()))
+            rounded += wide != Fraction(float(g.max())) - Fraction(float(g.min()))
+            want = next(c for c in scales if 15 * c >= wide)
+            zero = round(-Fraction(float(g.min())) / want)
+            assert Fraction(float(s[i, j])) == want and int(z[i, j]) == zero
+            assert codes[i, j].tolist() == [min(max(round(Fraction(float(v)) / want) + zero, 0), 15) for v in g]
+    assert rounded > 100
+    held = kv4_ref.values(codes, s, z)
+    assert bool(((held - x.double()).abs() <= s.repeat_interleave(32, -1) / 2).all())
+    assert float(kv4_ref.quantise(torch.tensor([15.0, -2.0 ** -30] + [0.0] * 126).to(torch.bfloat16))[1][0]) == 1
+
+
 def test_values_that_are_not_finite():
     x = torch.ones(3, 128, dtype=torch.bfloat16)
     x[0, 5], x[1, 40], x[2, 100] = float("nan"), float("inf"), float("-inf")
