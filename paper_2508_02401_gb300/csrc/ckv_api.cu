@@ -4,6 +4,7 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -2032,6 +2033,15 @@ Span rows_span(const void* p, int T, int heads, int64_t tok, int64_t head) {
     return {p, ((T - 1) * tok + (heads - 1) * head + kHeadDim) * 2};
 }
 
+// Whether a page of K and one of V share bytes: n pages of `bytes` each, `stride` bytes apart (>= bytes), V's `apart` bytes behind K's.
+bool pages_overlap(int64_t apart, int64_t n, int64_t stride, int64_t bytes) {
+    // page i of V and page i + m of K are apart - m stride apart: least at a quotient's two neighbours, where there are such pages
+    const int64_t m = apart / stride;
+    for (int64_t x = m - 1; x <= m + 1; ++x)
+        if (x > -n && x < n && std::abs(apart - x * stride) < bytes) return true;
+    return false;
+}
+
 // The appends: `L` has the cache's fields and q4.
 ckv_status enqueue_append(const ckv_config* cfg, AppendLaunch& L, int page_size, int num_pages, int32_t num_tokens,
                           const void* q, int64_t q_tok, int64_t q_head, void* q_out, const void* k, const void* v,
@@ -2071,17 +2081,20 @@ ckv_status enqueue_append(const ckv_config* cfg, AppendLaunch& L, int page_size,
     const Span in[] = {rows_span(q, T, Hq, q_tok, q_head), rows_span(k, T, Hkv, tok, head), rows_span(v, T, Hkv, tok, head),
                        {slot_map, 4ll * T}, {positions, 4ll * T},
                        {rot ? rot->cos_sin : nullptr, rot ? 4ll * rot->num_positions * rot->rotary_dim : 0}};
-    const int64_t pages = (num_pages - 1) * L.page_stride * (L.q4 ? 1 : 2) + static_cast<int64_t>(page_size) * Hkv * (L.q4 ? 144 : 256);
+    const int64_t page = static_cast<int64_t>(page_size) * Hkv * (L.q4 ? 144 : 256), apart = L.page_stride * (L.q4 ? 1 : 2);
+    const int64_t pages = (num_pages - 1) * apart + page;
+    if (!L.q4 && pages_overlap(reinterpret_cast<intptr_t>(L.v_pages) - reinterpret_cast<intptr_t>(L.k_pages), num_pages, apart, page))
+        return fail(CKV_ERR_INVALID_ARG, "pages of K lie over pages of V");
     const Span out[] = {rows_span(q_out, T, Hq, static_cast<int64_t>(Hq) * kHeadDim, kHeadDim),
                         rows_span(k_out, T, Hkv, static_cast<int64_t>(Hkv) * kHeadDim, kHeadDim),
                         rows_span(v_out, T, Hkv, static_cast<int64_t>(Hkv) * kHeadDim, kHeadDim),
-                        {L.k_pages, pages}, {L.v_pages, pages}};
-    for (int i = 0; i < 5; ++i) {
+                        {L.k_pages, pages}, {L.v_pages, pages}, {workspace, static_cast<int64_t>(l.total)}};
+    for (int i = 0; i < 6; ++i) {
         for (int j = 0; j < 6; ++j)
             if (overlap(out[i], in[j]) && !(i == j && i < 3 && out[i].p == in[j].p && (i == 0 ? q_packed : kv_packed)))
                 return fail(CKV_ERR_INVALID_ARG, "what the call writes lies over one of its inputs");
-        for (int j = i + 1; j < 5; ++j)  // (K's and V's pages may alternate in one buffer)
-            if (i < 3 && overlap(out[i], out[j])) return fail(CKV_ERR_INVALID_ARG, "two of the outputs overlap");
+        for (int j = i + 1; j < 6; ++j)  // (K's and V's pages may alternate in one buffer)
+            if (!(i == 3 && j == 4) && overlap(out[i], out[j])) return fail(CKV_ERR_INVALID_ARG, "two of the outputs overlap");
     }
     L.q = q;
     L.q_tok = q_tok;

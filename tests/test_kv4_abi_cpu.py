@@ -76,6 +76,30 @@ def test_append_writes_over_nothing(lib, q4, kw):
     assert _append(lib, q4, **kw) == 1
 
 
+_PAGE = 16 * 8 * 256  # bytes of a bf16 page of K
+
+
+@pytest.mark.parametrize("v_at,stride,pages", [
+    (_PAGES, 0, 10), (_PAGES + 16, 0, 10), (_PAGES + _PAGE - 16, 0, 1), (_PAGES - _PAGE + 16, 0, 1), (_PAGES + 3 * _PAGE, 0, 10),
+    (_PAGES + 9 * _PAGE, 0, 10), (_PAGES - 9 * _PAGE - 16, 0, 10), (_PAGES + _PAGE - 16, _PAGE, 10), (_PAGES + _PAGE + 16, _PAGE, 10),
+    (_PAGES + 2 * _PAGE, _PAGE, 10), (_PAGES + 3 * _PAGE - 16, _PAGE, 2), (_PAGES - 3 * _PAGE + 16, _PAGE, 2),
+])
+def test_append_refuses_pages_of_k_over_pages_of_v(lib, v_at, stride, pages):
+    assert _append(lib, False, cache=_cache(_PAGES, v_at, stride, pages)) == 1
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(k_out=_W), dict(q=_Q, q_out=_W - 16), dict(slots=_W), dict(pos=_W + 256), dict(k=_W + 1024), dict(v=_W - 256),
+    dict(q=_W, q_out=_QO), dict(rot=_rot(cs=_W - 64)),
+])
+def test_append_refuses_a_workspace_over_the_rest(lib, q4, kw):
+    assert _append(lib, q4, **kw) == 1
+    assert _append(lib, q4, cache=_cache4(_W - 16) if q4 else _cache(_W + 512, _VP)) == 1
+    if not q4:
+        assert _append(lib, q4, cache=_cache(_VP, _W)) == 1
+
+
 def test_append_q4_outputs(lib):
     for kw in (dict(v_out=_VO + 8), dict(v_out=_K), dict(k_out=_KO, v_out=_KO), dict(v_out=_V, tok=2048), dict(k_out=_V, v_out=_K)):
         assert _append(lib, True, **kw) == 1
@@ -121,3 +145,8 @@ def test_valid_calls_without_a_gpu_report_a_cuda_error(lib):
         assert _append(lib, q4, q=_Q, q_out=_Q, k_out=_K) == 4  # in place
     assert _append(lib, True, rot=None, pos=None, k_out=_K, v_out=_V) == 4
     assert _paged4(lib) == 4
+    # K's and V's pages side by side, alternating, or V's before K's
+    for v_at, stride, pages in ((_PAGES + 10 * _PAGE, 0, 10), (_PAGES - 10 * _PAGE, 0, 10), (_PAGES + _PAGE, _PAGE, 10),
+                                (_PAGES - _PAGE, _PAGE, 10), (_PAGES + 2 * _PAGE, 3 * _PAGE // 2, 10), (_PAGES + 4 * _PAGE, _PAGE, 2),
+                                (_PAGES + _PAGE, 0, 1)):
+        assert _append(lib, False, cache=_cache(_PAGES, v_at, stride, pages)) == 4
