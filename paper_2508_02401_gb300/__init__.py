@@ -140,7 +140,11 @@ def load():
         "ckv_paged_attention": ([cfg, cache, I32, I32, P, I32, P, P, P, I64, I64, P, P, I64, P, SZ, P], C.c_int),
     }
     for name, (args, res) in sigs.items():
-        fn = getattr(lib, name)
+        try:
+            fn = getattr(lib, name)
+        except AttributeError:
+            raise ImportError(f"{path} has no {name} (its ABI is version {lib.ckv_abi_version()}): it was built from older "
+                              "sources; build it again") from None
         fn.argtypes = args
         fn.restype = res
     _lib = lib

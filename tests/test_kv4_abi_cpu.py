@@ -150,3 +150,19 @@ def test_valid_calls_without_a_gpu_report_a_cuda_error(lib):
                                 (_PAGES - _PAGE, _PAGE, 10), (_PAGES + 2 * _PAGE, 3 * _PAGE // 2, 10), (_PAGES + 4 * _PAGE, _PAGE, 2),
                                 (_PAGES + _PAGE, 0, 1)):
         assert _append(lib, False, cache=_cache(_PAGES, v_at, stride, pages)) == 4
+
+
+def test_an_older_library_is_named(lib, monkeypatch):
+    """A library without one of the calls, though its version is the same: said when it is loaded, and nothing of it is kept."""
+
+    class Older:
+        def __getattr__(self, name):
+            if name == "ckv_cache_append_q4":
+                raise AttributeError(name)
+            return getattr(lib, name)
+
+    monkeypatch.setattr(ckv, "_lib", None)
+    monkeypatch.setattr(ckv.C, "CDLL", lambda path: Older())
+    with pytest.raises(ImportError, match="ckv_cache_append_q4.*version 7.*build"):
+        ckv.load()
+    assert ckv._lib is None
