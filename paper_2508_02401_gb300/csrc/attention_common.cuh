@@ -441,7 +441,7 @@ __device__ __forceinline__ void join_row(const AttnLaunch& a, const Item& I, int
                                        partial_of<ROWS>(a, I.cta0 + k0 + k + y, k0 + k + y == 0) + x * 128) + lane)
                                  : make_float4(0.f, 0.f, 0.f, 0.f);
         };
-        load(0);  // (beside the weights: 64 caches of 128 to 8192 in 4 bits 43.3 us without, 42.5 with)
+        load(0);  // (beside the weights: 64 caches of 128 to 8192 in 4 bits 43.3 us without, 42.5 with; in bf16 77.1 and 76.9)
         float pm = -INFINITY, pl = 0.f;
         if (lane < n) {
             const float* src = partial_of<ROWS>(a, I.cta0 + k0 + lane, k0 + lane == 0);

@@ -14,13 +14,14 @@
 // at half rate.  8 caches of 131072 tokens, one new token (4 rows a KV head, 1.21 GB): 269 us, 4.5 TB/s (a bf16 cache, 4.29 GB,
 // 623 us); the schedulers issue in 58 to 63% of the cycles, the rest is four warps' latencies.  With the differences, products
 // and masks left out (wrong results) a form of the loop took 241 us.  Legacy MMAs, since their operands come from registers, where the
-// codes are unpacked; of the tensor core's time 18% is used.  What else was built, us on those caches:
+// codes are unpacked; of the tensor core's time 18% is used.  What else was built, us on those caches, when the kernel took 286 (before
+// the loads in place of this step's and the joins' loads side by side; the prefetches when it took 274):
 //   tcgen05, keys on M: K unpacked into tensor memory, V into shared memory            425
 //   tcgen05 on the codes as 8-bit floats, numerators as pairs of those (too coarse)      339
 //   packed blocks by bulk copies into a ring of the CTA, scales behind the MMAs        305
 //   a ring of asynchronous copies for each warp                                        312
 //   8-bit-float MMAs for the logits                                                    334
-//   9 or 10 warps a CTA 327; one CTA of 16 warps 282 against 286, but 64 caches of 128 to 8192 74 against 50
+//   9 or 10 warps a CTA 327; one CTA of 16 warps 282, but 64 caches of 128 to 8192 74 against 50 then
 //   two steps a trip of the loop 288; a later step asked into L2, its rows 306, its pages by bulk prefetches 290
 //   s n in one fused operation, the zero points' part by MMAs of their own (fewer instructions, longer chains, and
 //   the small channels of a group with a large one cancel) 295
@@ -62,7 +63,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 // N8: blocks of 8 rows (1 or 2).
 template <int N8>
 struct FewSmem4 {
-    // 16 rows: 168 registers a thread, so six warps a CTA (40 sequences, 14 rows each, 49 us; one CTA of 12 warps 57).
+    // 16 rows: 168 registers a thread (and 40 bytes of spills), so six warps a CTA (40 sequences, 14 rows each, 49.5 us; one CTA of
+    // 12 warps 57).
     static constexpr int kWarps4 = N8 == 1 ? 8 : 6;
     static constexpr int kBufs = N8 == 1 ? 2 : 1;  // of the warps' outputs (two: no barrier after they are read)
     float o[kBufs][kWarps4][8 * N8][kPitch4];
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(32 * FewSmem4<N8>::kWarps4, kCtas4) attention_
         for (int i = 0; i < n; ++i) {
             // The next step's rows are loaded as soon as this one's are used, K's behind the logits and V's behind the output; with 16
             // rows, where fewer warps hide a load, now.  (8 caches of 131072 tokens, 4 rows, 275 us, 293 with all of them now; 40 of
-            // 512 to 16384, 14 rows, 54 and 51.)
+            // 512 to 16384, 14 rows, 54 and 51: both when the present 269 and 49.5 were 275 and 51.)
             Step here;
             if constexpr (N8 == 2) here = x;
             Step& cur = N8 == 2 ? here : x;
@@ -432,7 +434,7 @@ cudaError_t launch_attention_few_q4(const AttnLaunch& L, int rows, cudaStream_t 
     p.hp = p.G;
     p.tp = (rows <= 8 ? 8 : 16) / p.G;
     p.nhb = 1;
-    p.unit_cost = 2;  // key tiles (64 caches of 128 to 8192: 45.7 us; 1: 51.4, 3: 47.2, 6: 52.4)
+    p.unit_cost = 2;  // key tiles (64 caches of 128 to 8192, now 42.2 us, when they took 45.7: 1 51.4, 3 47.2, 6 52.4)
     p.min_run = 1;
     while ((1 << p.page_shift) < L.page_size) ++p.page_shift;
     p.c = L.scale * 1.4426950408889634f;

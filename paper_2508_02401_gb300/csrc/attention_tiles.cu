@@ -11,8 +11,8 @@
 // work 72% of the time; without its loads (a copy that skipped them) 1820.
 //
 // Over a cache of 4 bits (kPaged4) the packed tiles of 9 KB come by bulk copies into a ring of their own, and four more warps
-// make bf16 tiles of them, a row a thread; the rest is the same.  2048 new tokens over 32768 (32 / 8 heads): 1053 us,
-// 1075 TFLOP/s, against 732 over a bf16 cache: the unpacking warps' instructions take issue slots and shared memory from the softmax's.
+// make bf16 tiles of them, a row a thread; the rest is the same.  2048 new tokens over 32768 (32 / 8 heads): 1054 us,
+// 1074 TFLOP/s, against 732 over a bf16 cache: the unpacking warps' instructions take issue slots and shared memory from the softmax's.
 // With the codes stored without being unpacked (wrong results) it took 827, without the subtraction alone 977; other register
 // splits 1051 to 1081, two packed slots 1042, eight unpacking warps, K's and V's, with 168 / 48 / 48 registers 1165.
 #include <type_traits>

@@ -1717,12 +1717,19 @@ ckv_status enqueue_attention(AttnLaunch& L, cudaStream_t stream) {
     // among idle sequences (256 tokens, 255 idle: 692 / 49).
     const int64_t G = L.Hq / L.Hkv, T = L.T, S = L.S, rows = (T + S - 1) / S * G;
     // Over a cache of 4 bits, where the tile kernel unpacks a sequence's cache for every 256 rows, few / tiles: 8 sequences
-    // of 8000, 4 rows 30 / 84, 8 rows 31 / 82, 12 rows 39 / 84, 16 rows 40 / 82; 64 of 2000, 4 tokens each, 70 / 170; a chunk of
-    // 128 over 8000 among 64 single tokens 137 / 128, of 512 among 256 492 / 441; 64 tokens and 63 idle sequences 74 / 45.
-    // Up to 32 rows, which the few-rows kernel takes in two passes, where no sequence can have over 256: 8 of 8000 with 8 tokens
-    // each 62 / 82, one 25 / 39, of 131072 109 / 151 (with 12 155 / 158), 2 of 300 14.7 / 16.7; a chunk of 57 among 7 single
-    // tokens 79 / 89, but over 60000 with short ones beside it 333 / 117.  64 of 2000 with 8 tokens each, 121 / 170, stay with the
-    // tiles for the chunk of 449 that could be among them, 362 / 172.
+    // of 8000, 4 rows 30 / 84, 8 rows 31 / 82, 12 rows 39 / 84, 16 rows 40 / 82; 64 of 2000, 4 tokens each, 70 / 168, 256 225 / 606.
+    // At 16 rows whatever their spread, for the lengths are on the device and either choice is wrong for some mixture: what the
+    // tile kernel loses on the single tokens is 2.8 times at most, what the few-rows kernel loses on the chunk (its cache once for
+    // every 16 rows) is up to 6.  255 single tokens and a chunk of 769, all caches of 8000, 1285 / 2130, of 32768 5097 / 8103;
+    // of 512 over 1000 beside 8000 868 / 2036; 63 and a chunk of 128 over 8000 293 / 521.  But the chunk of 769 over 60000 beside
+    // caches of 2000 4213 / 1382, over 32768 2402 / 1012; of 512 over 131072 6011 / 1610; 15 single tokens over 2000 and 49 over
+    // 60000 302 / 129; 64 tokens of one sequence and 63 idle ones 77 / 45, over 60000 472 / 102.
+    // Up to 32 rows, which the few-rows kernel takes in two passes, where no sequence can have over 256 if all have a token: 8 of 8000
+    // with 8 tokens each 62 / 82, one 25 / 39, of 131072 109 / 151 (with 12 155 / 158), 2 of 300 14.7 / 16.7; a chunk of 57 among
+    // 7 single tokens 79 / 89, but over 60000 with short ones beside it 333 / 117.  64 of 2000 with 8 tokens each, 121 / 170, stay
+    // with the tiles for the chunk of 449 that could be among them, 362 / 172.  Where the others are idle one can have all: 16 heads a
+    // group, 1015 tokens over 60000 and 999 idle sequences 10494 / 1841.  A bound on all tokens would mend that and take 1000 single
+    // tokens and 15 rows of padding, 424 / 1159, along.
     const bool few = L.paged && (L.q4 ? rows <= 16 || (rows <= 32 && G <= 16 && (T - S + 1) * G <= 256)
                                       : rows <= 16 && (T <= 2 * S || (T - S + 1) * G <= 64));
     CUtensorMap mq, mk{}, mv{};  // (a cache of 4 bits has no maps)

@@ -9,7 +9,7 @@
 //
 // In a page of P tokens, per head: K's codes [4 groups][P][16 bytes], K's scales [P][4 groups][2 bytes], then V's.  A
 // group's 16 bytes are four words of 8 channels, channel c of a word in nibble c / 2 + 4 (c % 2), so that a mask of
-// two nibbles gives a pair of neighbours.  A scale is its bf16 pattern, whose low nibble is free: z.
+// two nibbles gives a pair of neighbours (a mask and a magic exponent: a published technique of 4-bit kernels).  A scale is its bf16 pattern, whose low nibble is free: z.
 #pragma once
 
 #include <float.h>
